@@ -453,6 +453,113 @@ acid_status acid_block_forward(acid_model* m, int32_t block,
                                const float* mod6_dev, float* h_dev,
                                hipStream_t stream);
 
+/* ---------------- the linear-attention block: prompts and single tokens */
+
+/* Causal linear attention with a decay for each head, lambda_h =
+ * exp(-slopes_dev[h]), slopes >= 0 (0: no decay), over n_seq sequences:
+ *   S_t = lambda S_{t-1} + k_t^T v_t   (S_{-1}: state_in, or 0 if NULL)
+ *   o_t = scale q_t S_t
+ * q, k: [n_seq][n_heads][L][d]; vt: V transposed, [n_seq][n_heads][d][vt_ld]
+ * with vt_ld >= round_up(L, 8), a multiple of 8 (the layout the QKV epilogue
+ * writes and acid_attention reads); o: [n_seq][L][n_heads*d]; all in `dtype`.
+ * States: fp32 [n_seq][n_heads][d][d], row i over k's column i; state_out
+ * (NULL: not wanted) may be state_in itself.  lengths_dev (NULL: all L):
+ * sequence b has lengths[b] tokens, clamped to [0, L]; what the padding holds
+ * is never used, its rows of o are left as they are, and the state is the
+ * one after the last token (state_in, or 0, for none).  d is 64 or 128.
+ * Products are accumulated, and states kept, in fp32.  q, k, v and the state
+ * must be finite: a NaN or an infinity spoils its head's outputs from 63
+ * tokens before it on.
+ * Workspace: acid_linear_attention_workspace_bytes(...) bytes (0: may be
+ * NULL), 16-byte aligned, not shared by calls that may overlap; ACID_ERR_SHAPE
+ * if it is smaller.  Buffers 16-byte aligned, outputs apart from inputs. */
+size_t acid_linear_attention_workspace_bytes(int64_t n_seq, int32_t n_heads,
+                                             int64_t seq_len, int32_t head_dim);
+acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
+                                  int64_t seq_len, int32_t head_dim,
+                                  const void* q_dev, const void* k_dev,
+                                  const void* vt_dev, int64_t vt_ld,
+                                  const float* slopes_dev,
+                                  const int32_t* lengths_dev,
+                                  const float* state_in_dev, float* state_out_dev,
+                                  float scale, void* o_dev, void* workspace_dev,
+                                  size_t workspace_bytes, hipStream_t stream);
+
+/* The same recurrence, one token a row: row i takes its state from slot
+ * slots_dev[i] (NULL: slot i) of state_in, fp32 [n_slots][n_heads][d][d], and
+ * leaves the new one in that slot of state_out (state_in itself, or a buffer
+ * apart, whose other slots are left as they are).  A slot outside [0, n_slots)
+ * marks a padding row: nothing of it is read or written.  Rows with the same
+ * slot are one sequence's successive tokens, in row order.  q, k, v, o: rows
+ * of n_heads*d in `dtype`, *_ld elements apart (whole 16 bytes): columns
+ * h*d .. (h+1)*d belong to head h, as in a projection's Q | K | V. */
+acid_status acid_linear_attention_step(int32_t dtype, int64_t n_rows, int32_t n_heads,
+                                       int32_t head_dim, const void* q_dev, int64_t q_ld,
+                                       const void* k_dev, int64_t k_ld,
+                                       const void* v_dev, int64_t v_ld,
+                                       const float* slopes_dev, const int32_t* slots_dev,
+                                       int64_t n_slots, const float* state_in_dev,
+                                       float* state_out_dev, float scale, void* o_dev,
+                                       int64_t o_ld, hipStream_t stream);
+
+/* LAYER: (x - mean) / sqrt(var + eps), biased variance; RMS:
+ * x / sqrt(mean(x^2) + eps). */
+typedef enum { ACID_NORM_NONE = 0, ACID_NORM_LAYER = 1, ACID_NORM_RMS = 2 } acid_norm_kind;
+
+typedef struct {
+  const float* h;            /* residual stream */
+  int64_t h_ld;
+  const void* y;             /* the block's output in y_dtype; NULL: none yet */
+  int64_t y_ld;
+  float* h_out;              /* h itself (same stride) or apart; with y only */
+  int64_t h_out_ld;
+  void* out;                 /* the next block's input in out_dtype; NULL: not wanted */
+  int64_t out_ld;
+  int32_t y_dtype, out_dtype;
+  int32_t post, pre;         /* acid_norm_kind of y and of h_out */
+  const float* post_weight;  /* [hidden], NULL: 1 */
+  const float* pre_weight;   /* [hidden], NULL: 1 */
+  const float* gate;         /* [n_mod][hidden], NULL: 1 */
+  const float* shift;        /* [n_mod][hidden], NULL: 0 */
+  const float* scale;        /* [n_mod][hidden], NULL: 0 */
+  int64_t rows_per_mod;      /* rows that share a modulation row; 0: all */
+  float res_scale, eps;
+} acid_residual_norm_args;
+
+/* The seam between two blocks, one pass over the rows:
+ *   h_out = res_scale h + gate (N_post(y) post_weight)
+ *   out   = (N_pre(h_out) pre_weight) (1 + scale) + shift
+ * (without y, out is made from h itself).  Row r uses row r / rows_per_mod of
+ * gate, shift and scale.  h, h_out and statistics fp32.  hidden % 4 == 0,
+ * <= 16384; rows <= 2^23; row strides in elements, multiples of 4; matrices
+ * aligned to four of their elements, vectors to 16 bytes; outputs apart from
+ * everything but h_out from h (columns of one matrix may interleave). */
+acid_status acid_residual_norm(const acid_residual_norm_args* args, int64_t rows,
+                               int32_t hidden, hipStream_t stream);
+
+/* 4-bit weights: w[n][k] = (c[n][k] - 8) scales[n][k / group], c in 0..15,
+ * group 32, 64 or 128, K a multiple of 128, K and N <= 2^22.  Outputs are laid
+ * out in tiles of 16, the last one padded:
+ *   codes  [ceil(N/16)][K/128][64][16 bytes]: run l of a tile's 128 inputs is
+ *          output l % 16; its 32-bit word j holds inputs 32 j + 8 (l / 16) +
+ *          (0, 2, 4, 6, 1, 3, 5, 7) in its nibbles from the lowest up
+ *   scales fp32 [ceil(N/16)][K/group][16]
+ * acid_quantize_w4 fills both (padding included) from fp32 [K][N] ([in][out],
+ * as the manifest has it): scale = max |w| / 7 over the group, code = w / scale
+ * to nearest even, + 8; a group with a NaN or an infinity gets scale NaN. */
+acid_status acid_quantize_w4(const float* w_dev, int32_t N, int32_t K, int32_t group,
+                             void* codes_dev, float* scales_dev, hipStream_t stream);
+
+/* out = act(x w^T + bias) for few rows (meant for up to 64; at most 65536): x
+ * [M][x_ld] in x_dtype, whole 16 bytes apart; out [M][out_ld] in out_dtype;
+ * bias fp32 [N] or NULL; kind ACID_EPI_BIAS or ACID_EPI_BIAS_GELU.  fp32 rows
+ * are not rounded; accumulation fp32.  |x| < 2^120. */
+acid_status acid_linear_w4(int32_t x_dtype, int64_t M, int32_t N, int32_t K, int32_t group,
+                           const void* x_dev, int64_t x_ld, const void* codes_dev,
+                           const float* scales_dev, const float* bias_dev, int32_t kind,
+                           int32_t out_dtype, void* out_dev, int64_t out_ld,
+                           hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,12 +17,13 @@ from ._lib import (ACID_BF16, ACID_CACHE_APPLY, ACID_CACHE_STORE, ACID_EPI_BIAS,
                    ACID_EPI_BIAS_GELU, ACID_EPI_EULER, ACID_EPI_GATE_RESIDUAL, ACID_EPI_QKV,
                    ACID_EPI_QKV_GELU, ACID_BLOCK_PARALLEL, ACID_BLOCK_SEQUENTIAL,
                    ACID_F32, ACID_MODE_ACID, ACID_MODE_DICACHE, ACID_MODE_EASYCACHE,
-                   ACID_MODE_NOCACHE,
+                   ACID_MODE_NOCACHE, ACID_NORM_LAYER, ACID_NORM_NONE, ACID_NORM_RMS,
                    KERNEL_CLASSES, AcidError,
                    TRACE_DTYPE, check, lib)
 
 __all__ = ["Model", "gate", "GateState", "gate_device_sequence", "cache_apply", "easycache_reuse", "attention", "linear",
-           "ln_modulate", "q_scale", "version", "AcidError", "KERNEL_CLASSES"]
+           "ln_modulate", "linear_attention", "linear_attention_step", "linear_attention_workspace",
+           "linear_w4", "quantize_w4", "w4_shapes", "residual_norm", "q_scale", "version", "AcidError", "KERNEL_CLASSES"]
 
 
 def _torch():
@@ -167,6 +168,237 @@ def linear(a, wt, kind: int, bias, gate=None, out=None, v_out=None, q=None, k=No
     e.n_heads, e.head_dim, e.dsigma = n_heads, head_dim, dsigma
     e.q_prescale = int(bool(q_prescale))
     check(lib().acid_linear(code, M, N, K, _ptr(a), _ptr(wt), C.byref(e), _stream(stream)))
+
+
+# ------------------------------------------------ linear-attention block
+
+
+def _dtype_code(t, name: str) -> int:
+    torch = _torch()
+    if t.dtype == torch.bfloat16:
+        return ACID_BF16
+    if t.dtype == torch.float32:
+        return ACID_F32
+    raise ValueError(f"{name}: expected bfloat16 or float32, got {t.dtype}")
+
+
+def _expect(device, name: str, t, shape, dtype) -> None:
+    """t (if given) is a contiguous device tensor of this shape and type."""
+    if t is None:
+        return
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name}: expected a tensor on {device}, got {t.device}")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)}, "
+                         f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _rows(device, name: str, t, rows: int, cols: int):
+    """(address, row stride) of a [rows, cols] device tensor of unit column
+    stride; a row stride that no row uses is given as whole rows."""
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name}: expected a tensor on {device}, got {t.device}")
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: expected unit column stride, got {t.stride()}")
+    if rows > 1 and t.stride(0) < cols:
+        raise ValueError(f"{name}: rows overlap (strides {t.stride()})")
+    return C.c_void_p(t.data_ptr()), (t.stride(0) if rows > 1 else (cols + 7) // 8 * 8)
+
+
+def _stream_of(device, stream):
+    """The stream a call on `device` runs on: the one given, which has to be
+    that device's, or the device's current one."""
+    s = stream if stream is not None else _torch().cuda.current_stream(device)
+    if s.device != device:
+        raise ValueError(f"stream of {s.device} for tensors on {device}")
+    return s
+
+
+def linear_attention_workspace(n_seq: int, n_heads: int, seq_len: int, head_dim: int) -> int:
+    """Bytes of workspace linear_attention needs for these sizes."""
+    return int(lib().acid_linear_attention_workspace_bytes(n_seq, n_heads, seq_len, head_dim))
+
+
+def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths=None,
+                     scale: Optional[float] = None, workspace=None, stream=None) -> None:
+    """Causal linear attention, S_t = exp(-slope) S_{t-1} + k_t^T v_t and o_t =
+    scale q_t S_t (scale defaults to 1/sqrt(d)).  q, k [n_seq, heads, L, d];
+    vt [n_seq, heads, d, vt_ld]; o [n_seq, L, heads*d]; all bf16 or all fp32
+    (attention's layouts; without the n_seq axis for one sequence).  slopes
+    fp32 [heads]; states fp32 [n_seq, heads, d, d], state_out may be state_in;
+    lengths int32 [n_seq]: tokens of each sequence, its later rows of o are
+    left as they are.  workspace: uint8 tensor of linear_attention_workspace
+    bytes, kept by callers whose calls must not allocate; by default one is
+    taken from torch's allocator for the call."""
+    torch = _torch()
+    if q.dim() not in (3, 4):
+        raise ValueError("q: expected [heads, L, d] or [n_seq, heads, L, d]")
+    code, dev, lead = _dtype_code(q, "q"), q.device, tuple(q.shape[:-3])
+    n_heads, L, d = q.shape[-3:]
+    n_seq = lead[0] if lead else 1
+    if vt.dim() != q.dim():
+        raise ValueError("vt: expected as many axes as q")
+    _expect(dev, "q", q, q.shape, q.dtype)
+    _expect(dev, "k", k, q.shape, q.dtype)
+    _expect(dev, "vt", vt, lead + (n_heads, d, vt.shape[-1]), q.dtype)
+    _expect(dev, "o", o, lead + (L, n_heads * d), q.dtype)
+    _expect(dev, "slopes", slopes, (n_heads,), torch.float32)
+    for name, t in (("state_in", state_in), ("state_out", state_out)):
+        _expect(dev, name, t, lead + (n_heads, d, d), torch.float32)
+    _expect(dev, "lengths", lengths, (n_seq,), torch.int32)
+    s = _stream_of(dev, stream)
+    if workspace is None:
+        need = linear_attention_workspace(n_seq, n_heads, L, d)
+        if need:
+            with torch.cuda.stream(s):  # its memory goes back to this stream's pool
+                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    elif workspace.dtype != torch.uint8:
+        raise ValueError("workspace: expected a uint8 tensor")
+    else:
+        _expect(dev, "workspace", workspace, workspace.shape, torch.uint8)
+    check(lib().acid_linear_attention(
+        code, n_seq, n_heads, L, d, _ptr(q), _ptr(k), _ptr(vt), vt.shape[-1], _ptr(slopes),
+        _ptr(lengths), _ptr(state_in), _ptr(state_out),
+        float(d ** -0.5 if scale is None else scale), _ptr(o), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), C.c_void_p(s.cuda_stream)))
+
+
+def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
+                          scale: Optional[float] = None, stream=None) -> None:
+    """linear_attention's recurrence, one token a row.  q, k, v, o [rows,
+    heads*d], unit column stride (columns of one projection's output will do);
+    state fp32 [n_slots, heads, d, d], updated in place unless state_out is
+    given; slots int32 [rows]: each row's state (default: its own index), any
+    value outside [0, n_slots) marking a padding row that is left alone; rows
+    of one slot are successive tokens, in row order."""
+    torch = _torch()
+    if state.dim() != 4:
+        raise ValueError("state: expected [n_slots, heads, d, d]")
+    code, dev = _dtype_code(q, "q"), state.device
+    n_slots, n_heads, d, _ = state.shape
+    rows = q.shape[0]
+    out = state if state_out is None else state_out
+    _expect(dev, "state", state, (n_slots, n_heads, d, d), torch.float32)
+    _expect(dev, "state_out", out, (n_slots, n_heads, d, d), torch.float32)
+    _expect(dev, "slopes", slopes, (n_heads,), torch.float32)
+    _expect(dev, "slots", slots, (rows,), torch.int32)
+    args = []
+    for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
+        if t.dtype != q.dtype:
+            raise ValueError(f"{name}: expected {q.dtype}, got {t.dtype}")
+        args.append(_rows(dev, name, t, rows, n_heads * d))
+    s = _stream_of(dev, stream)
+    check(lib().acid_linear_attention_step(
+        code, rows, n_heads, d, *args[0], *args[1], *args[2], _ptr(slopes), _ptr(slots), n_slots,
+        _ptr(state), _ptr(out), float(d ** -0.5 if scale is None else scale), *args[3],
+        C.c_void_p(s.cuda_stream)))
+
+
+_NORMS = {"none": ACID_NORM_NONE, "layer": ACID_NORM_LAYER, "rms": ACID_NORM_RMS}
+
+
+def residual_norm(h, y=None, h_out=None, out=None, res_scale: float = 1.0, post: str = "none",
+                  post_weight=None, gate=None, pre: str = "layer", pre_weight=None, shift=None,
+                  scale=None, rows_per_mod: int = 0, eps: float = 1e-6, stream=None) -> None:
+    """Between two blocks, in one pass: h_out = res_scale h + gate (N_post(y)
+    post_weight), then out = (N_pre(h_out) pre_weight) (1 + scale) + shift.
+    h, h_out fp32 [rows, hidden] (h_out defaults to h, in place); y, out bf16
+    or fp32, either may be None; norms "none", "layer" or "rms"; weights fp32
+    [hidden]; gate, shift, scale fp32 [hidden], or [n_mod, hidden] with row r
+    using row r // rows_per_mod.  Matrices may be row-strided."""
+    torch = _torch()
+    if h.dim() != 2 or h.dtype != torch.float32:
+        raise ValueError("h: expected an fp32 [rows, hidden] tensor")
+    for kind in (post, pre):
+        if kind not in _NORMS:
+            raise ValueError(f"unknown norm {kind!r}")
+    if rows_per_mod < 0:
+        raise ValueError("rows_per_mod < 0")
+    dev, (rows, hidden) = h.device, h.shape
+    if y is None and h_out is not None:
+        raise ValueError("h_out without y")
+    if h_out is None:
+        h_out = h
+    elif h_out.dtype != torch.float32:
+        raise ValueError("h_out: expected fp32")
+    a = _L.ResidualNormArgsC()
+    a.h, a.h_ld = _rows(dev, "h", h, rows, hidden)
+    if y is not None:
+        a.y_dtype = _dtype_code(y, "y")
+        a.y, a.y_ld = _rows(dev, "y", y, rows, hidden)
+        a.h_out, a.h_out_ld = _rows(dev, "h_out", h_out, rows, hidden)
+    if out is not None:
+        a.out_dtype = _dtype_code(out, "out")
+        a.out, a.out_ld = _rows(dev, "out", out, rows, hidden)
+    n_mod = -(-rows // rows_per_mod) if rows_per_mod else 1
+    for name, t in (("post_weight", post_weight), ("pre_weight", pre_weight)):
+        _expect(dev, name, t, (hidden,), torch.float32)
+    for name, t in (("gate", gate), ("shift", shift), ("scale", scale)):
+        if t is not None and t.dim() == 1 and n_mod == 1:
+            _expect(dev, name, t, (hidden,), torch.float32)
+        else:
+            _expect(dev, name, t, (n_mod, hidden), torch.float32)
+    a.post_weight, a.pre_weight = _ptr(post_weight), _ptr(pre_weight)
+    a.gate, a.shift, a.scale = _ptr(gate), _ptr(shift), _ptr(scale)
+    a.post, a.pre = _NORMS[post], _NORMS[pre]
+    a.rows_per_mod, a.res_scale, a.eps = int(rows_per_mod), float(res_scale), float(eps)
+    s = _stream_of(dev, stream)
+    check(lib().acid_residual_norm(C.byref(a), rows, hidden, C.c_void_p(s.cuda_stream)))
+
+
+def w4_shapes(n: int, k: int, group: int = 128):
+    """Shapes of the codes (uint8) and scales (fp32) of an [n outputs, k
+    inputs] 4-bit weight; see include/acid.h for what they hold."""
+    if n < 1 or k < 128 or k % 128 or group not in (32, 64, 128):
+        raise ValueError("n >= 1, k a multiple of 128, group 32, 64 or 128")
+    tiles = -(-n // 16)
+    return (tiles, k // 128, 64, 16), (tiles, k // group, 16)
+
+
+def _w4_group(codes, scales, k: int):
+    if codes.dim() != 4 or scales.dim() != 3 or scales.shape[1] < 1 or k % scales.shape[1]:
+        raise ValueError("codes, scales: see w4_shapes")
+    return k // scales.shape[1]
+
+
+def quantize_w4(w, codes, scales, stream=None) -> None:
+    """codes, scales (w4_shapes) of the fp32 weight w [k inputs, n outputs]."""
+    torch = _torch()
+    if w.dim() != 2:
+        raise ValueError("w: expected [k, n]")
+    (k, n), dev = w.shape, w.device
+    group = _w4_group(codes, scales, k)
+    cs, ss = w4_shapes(n, k, group)
+    _expect(dev, "w", w, (k, n), torch.float32)
+    _expect(dev, "codes", codes, cs, torch.uint8)
+    _expect(dev, "scales", scales, ss, torch.float32)
+    s = _stream_of(dev, stream)
+    check(lib().acid_quantize_w4(_ptr(w), n, k, group, _ptr(codes), _ptr(scales),
+                                 C.c_void_p(s.cuda_stream)))
+
+
+def linear_w4(x, codes, scales, out, bias=None, gelu: bool = False, stream=None) -> None:
+    """out = act(x w^T + bias) for few rows x [m, k] (bf16 or fp32) and 4-bit
+    weights (quantize_w4); out [m, n] bf16 or fp32; bias fp32 [n].  x and out
+    may be row-strided."""
+    torch = _torch()
+    if x.dim() != 2 or out.dim() != 2:
+        raise ValueError("x and out: expected two axes")
+    (m, k), n, dev = x.shape, out.shape[1], x.device
+    group = _w4_group(codes, scales, k)
+    cs, ss = w4_shapes(n, k, group)
+    _expect(dev, "codes", codes, cs, torch.uint8)
+    _expect(dev, "scales", scales, ss, torch.float32)
+    _expect(dev, "bias", bias, (n,), torch.float32)
+    xp, x_ld = _rows(dev, "x", x, m, k)
+    op, out_ld = _rows(dev, "out", out, m, n)
+    s = _stream_of(dev, stream)
+    check(lib().acid_linear_w4(_dtype_code(x, "x"), m, n, k, group, xp, x_ld, _ptr(codes),
+                               _ptr(scales), _ptr(bias),
+                               ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS,
+                               _dtype_code(out, "out"), op, out_ld, C.c_void_p(s.cuda_stream)))
 
 
 # ------------------------------------------------------------------ model

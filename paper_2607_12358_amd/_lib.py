@@ -24,6 +24,7 @@ ACID_CACHE_STORE, ACID_CACHE_APPLY = 0, 1
 (ACID_EPI_BIAS, ACID_EPI_BIAS_GELU, ACID_EPI_GATE_RESIDUAL, ACID_EPI_QKV,
  ACID_EPI_EULER, ACID_EPI_QKV_GELU) = range(6)
 ACID_BLOCK_SEQUENTIAL, ACID_BLOCK_PARALLEL = 0, 1
+ACID_NORM_NONE, ACID_NORM_LAYER, ACID_NORM_RMS = 0, 1, 2
 KERNEL_CLASSES = ("temb", "ln_mod", "gemm_qkv", "attention", "gemm_proj", "gemm_ffn1",
                   "gemm_ffn2", "gemm_head", "drift", "cache", "misc")
 
@@ -63,6 +64,17 @@ class EpilogueArgsC(C.Structure):
                 ("k", C.c_void_p), ("vt", C.c_void_p), ("vt_ld", C.c_int64),
                 ("n_heads", C.c_int32), ("head_dim", C.c_int32), ("dsigma", C.c_float),
                 ("q_prescale", C.c_int32)]
+
+
+class ResidualNormArgsC(C.Structure):
+    _fields_ = [("h", C.c_void_p), ("h_ld", C.c_int64), ("y", C.c_void_p), ("y_ld", C.c_int64),
+                ("h_out", C.c_void_p), ("h_out_ld", C.c_int64),
+                ("out", C.c_void_p), ("out_ld", C.c_int64),
+                ("y_dtype", C.c_int32), ("out_dtype", C.c_int32),
+                ("post", C.c_int32), ("pre", C.c_int32),
+                ("post_weight", C.c_void_p), ("pre_weight", C.c_void_p), ("gate", C.c_void_p),
+                ("shift", C.c_void_p), ("scale", C.c_void_p), ("rows_per_mod", C.c_int64),
+                ("res_scale", C.c_float), ("eps", C.c_float)]
 
 
 _P = C.c_void_p
@@ -105,6 +117,18 @@ _SIGS = {
                                  C.c_int64, _P, C.c_int32, _P]),
     "acid_linear": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, C.c_int32, _P, _P,
                               C.POINTER(EpilogueArgsC), _P]),
+    "acid_linear_attention_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int64,
+                                                           C.c_int32]),
+    "acid_linear_attention": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_int32,
+                                        _P, _P, _P, C.c_int64, _P, _P, _P, _P, C.c_float, _P, _P,
+                                        C.c_size_t, _P]),
+    "acid_linear_attention_step": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, C.c_int32,
+                                             _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, _P,
+                                             C.c_int64, _P, _P, C.c_float, _P, C.c_int64, _P]),
+    "acid_residual_norm": (C.c_int, [C.POINTER(ResidualNormArgsC), C.c_int64, C.c_int32, _P]),
+    "acid_quantize_w4": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]),
+    "acid_linear_w4": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, _P,
+                                 C.c_int64, _P, _P, _P, C.c_int32, C.c_int32, _P, C.c_int64, _P]),
     "acid_block_forward": (C.c_int, [_P, C.c_int32, _P, _P, _P]),
 }
 

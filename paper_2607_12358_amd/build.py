@@ -23,7 +23,7 @@ LIB = os.path.join(PKG, "libacid.so")
 ARCH = "gfx950"
 
 HIP_SOURCES = ["elementwise.hip", "temb.hip", "gemm.hip", "attention.hip", "runtime.hip",
-               "noalloc.hip"]
+               "noalloc.hip", "linear_attention.hip", "residual_norm.hip", "linear_w4.hip"]
 HOST_SOURCES = ["gate.cpp"]
 
 

@@ -63,6 +63,47 @@ inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 // QKV epilogue can store Q pre-multiplied by it (the same float value).
 inline float attn_q_scale(int d) { return 1.4426950408889634f / sqrtf((float)d); }
 
+// Makes a stream's device current while an entry point launches on it, and
+// the caller's again after.  (The null stream belongs to the current device.)
+class StreamDevice {
+ public:
+  ~StreamDevice() {
+    if (was_ >= 0) (void)hipSetDevice(was_);
+  }
+  acid_status enter(hipStream_t s) {
+    if (!s) return ACID_OK;
+    int cur = 0, dev = 0;
+    ACID_HIP(hipGetDevice(&cur));
+    ACID_HIP(hipStreamGetDevice(s, &dev));
+    if (dev == cur) return ACID_OK;
+    ACID_HIP(hipSetDevice(dev));
+    was_ = cur;
+    return ACID_OK;
+  }
+
+ private:
+  int was_ = -1;
+};
+
+// Whether two row-strided buffers (rows of `width` bytes, `ld` bytes apart)
+// share a byte.  Buffers of one row stride may interleave, as column ranges
+// of one matrix do; of different strides they may not.
+inline bool rows_overlap(const void* a, int64_t a_rows, int64_t a_width, int64_t a_ld,
+                         const void* b, int64_t b_rows, int64_t b_width, int64_t b_ld) {
+  if (!a || !b || a_rows < 1 || b_rows < 1 || a_width < 1 || b_width < 1) return false;
+  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
+  const uintptr_t a1 = a0 + (uintptr_t)((a_rows - 1) * a_ld + a_width);
+  const uintptr_t b1 = b0 + (uintptr_t)((b_rows - 1) * b_ld + b_width);
+  if (a1 <= b0 || b1 <= a0) return false;
+  if (a_ld != b_ld || a_ld == 0) return true;
+  const int64_t gap = b0 >= a0 ? (int64_t)((b0 - a0) % (uintptr_t)a_ld)
+                               : (a_ld - (int64_t)((a0 - b0) % (uintptr_t)a_ld)) % a_ld;
+  return gap < a_width || gap + b_width > a_ld;  // b starts inside a's row, or runs into the next
+}
+inline bool bytes_overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  return rows_overlap(a, 1, a_bytes, a_bytes, b, 1, b_bytes, b_bytes);
+}
+
 // ---------------------------------------------------------------- launchers
 // Each returns hipGetLastError() of its launch.
 

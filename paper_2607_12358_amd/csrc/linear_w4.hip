@@ -1,0 +1,322 @@
+// Few rows times 4-bit weights with group scales (acid_linear_w4), and the
+// conversion of fp32 weights to them (acid_quantize_w4).
+//
+//   out[m][n] = act(sum_k x[m][k] (c[n][k] - 8) s[n][k / group] + bias[n])
+//
+// Bound by reading the codes once (HBM), so the layout is the one the matrix
+// instruction takes: a tile is 16 outputs x 128 inputs, 1 KB, and lane l of
+// the wave that reads it gets the 16 bytes of output l % 16 whose word j
+// holds inputs 32 j + 8 (l / 16) .. + 7, its share of the j-th 16x16x32
+// product.  Nibbles 0-3 and 4-7 of a word are its even and odd inputs, so
+// one shift and one and-or turn two of them into a register pair of bf16.
+#include <cfloat>
+#include <cmath>
+#include <type_traits>
+
+#include "common.h"
+
+namespace acid {
+namespace {
+
+// The eight codes of a word as bf16 values 16 + c: c sits in the top four
+// mantissa bits of 16.0 (0x4180), exact.
+__device__ __forceinline__ bf16x8 decode(uint32_t w) {
+  u32x4 r;
+  r[0] = ((w << 3) & 0x00780078u) | 0x41804180u;
+  r[1] = ((w >> 1) & 0x00780078u) | 0x41804180u;
+  r[2] = ((w >> 5) & 0x00780078u) | 0x41804180u;
+  r[3] = ((w >> 9) & 0x00780078u) | 0x41804180u;
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// Eight inputs of one operand row.  bf16 rows are taken as they are.  An
+// fp32 row becomes three operand rows: the value cut to its first eight
+// significant bits, the next eight, and the rest; their sum is exact, and the
+// three products are added at the end.
+__device__ __forceinline__ bf16x8 load_x(const bf16* p, int) {
+  return *reinterpret_cast<const bf16x8*>(p);
+}
+__device__ __forceinline__ bf16x8 load_x(const float* p, int part) {
+  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+  uint32_t u[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = i < 4 ? a[i & 3] : b[i & 3];
+    const float p0 = __uint_as_float(__float_as_uint(v) & 0xffff0000u), r = v - p0;
+    const float p1 = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+    u[i] = __float_as_uint(part == 0 ? p0 : part == 1 ? p1 : r - p1);
+  }
+  u32x4 out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = __builtin_amdgcn_perm(u[2 * i + 1], u[2 * i], 0x07060302u);
+  return __builtin_bit_cast(bf16x8, out);
+}
+
+struct W4Args {
+  const void* x;
+  const uint8_t* codes;
+  const float* scales;
+  const float* bias;
+  void* out;
+  int64_t x_ld, out_ld;
+  int32_t M, N, K, gelu;
+};
+
+// A workgroup owns NT tiles of outputs and MT tiles of operand rows; its
+// waves take the 128-input blocks in turn and their sums are added in wave
+// order.  The matrix products give sum x (16 + c); one more product with the
+// constant -24, shared by the output tiles, makes that sum x (c - 8) before
+// the group's scale.
+template <typename X, typename Out, int GROUP, int NT, int MT>
+__global__ __launch_bounds__(512) void linear_w4_kernel(W4Args a) {
+  constexpr int RPT = std::is_same_v<X, float> ? 5 : 16;  // rows of a row tile
+  extern __shared__ float red[];                          // [wave][mt][nt][16][16]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int col = lane & 15, g = lane >> 4;
+  const int KB = a.K / 128, tiles = (a.N + 15) / 16;
+  const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * (MT * RPT);
+  const int part = std::is_same_v<X, float> ? col % 3 : 0;
+
+  const X* x[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    int m = m0 + mt * RPT + (std::is_same_v<X, float> ? (col < 15 ? col / 3 : 4) : col);
+    m = m < a.M ? m : a.M - 1;  // rows past the end: copies whose results are dropped
+    x[mt] = (const X*)a.x + m * a.x_ld + 8 * g;
+  }
+  const u32x4* codes[NT];
+  const float* scales[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int64_t t = tile0 + nt < tiles ? tile0 + nt : tiles - 1;
+    codes[nt] = reinterpret_cast<const u32x4*>(a.codes) + t * KB * 64 + lane;
+    scales[nt] = a.scales + t * (a.K / GROUP) * 16 + col;
+  }
+  bf16x8 minus24;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) minus24[i] = (bf16)-24.0f;
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  for (int b = wave; b < KB; b += waves) {
+    u32x4 c[NT];
+    float s[NT][128 / GROUP];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      c[nt] = codes[nt][b * 64];
+#pragma unroll
+      for (int i = 0; i < 128 / GROUP; ++i) s[nt][i] = scales[nt][(b * (128 / GROUP) + i) * 16];
+    }
+    f32x4 off[MT], sum[MT][NT];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool first = j * 32 % GROUP == 0, last = (j + 1) * 32 % GROUP == 0;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const bf16x8 xf = load_x(x[mt] + b * 128 + 32 * j, part);
+        off[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            xf, minus24, first ? f32x4{0.f, 0.f, 0.f, 0.f} : off[mt], 0, 0, 0);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          sum[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              xf, decode(c[nt][j]), first ? f32x4{0.f, 0.f, 0.f, 0.f} : sum[mt][nt], 0, 0, 0);
+        }
+        if (last) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc[mt][nt][i] =
+                  fmaf(s[nt][j * 32 / GROUP], sum[mt][nt][i] + off[mt][i], acc[mt][nt][i]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        red[((wave * MT + mt) * NT + nt) * 256 + (4 * g + i) * 16 + col] = acc[mt][nt][i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < MT * NT * RPT * 16; i += blockDim.x) {
+    const int c = i % 16, nt = i / 16 % NT, r = i / 16 / NT % RPT, mt = i / 16 / NT / RPT;
+    const int n = (tile0 + nt) * 16 + c, m = m0 + mt * RPT + r;
+    if (n >= a.N || m >= a.M) continue;
+    float y = 0.f;
+    for (int w = 0; w < waves; ++w) {
+      const float* p = red + ((w * MT + mt) * NT + nt) * 256 + c;
+      if constexpr (std::is_same_v<X, float>)
+        y += (p[(3 * r + 2) * 16] + p[(3 * r + 1) * 16]) + p[3 * r * 16];
+      else
+        y += p[r * 16];
+    }
+    if (a.bias) y += a.bias[n];
+    if constexpr (std::is_same_v<Out, bf16>) {
+      if (a.gelu) y = gelu_tanh_fast(y);
+    } else {
+      if (a.gelu) y = gelu_tanh(y);
+    }
+    ((Out*)a.out)[m * a.out_ld + n] = (Out)y;
+  }
+}
+
+template <typename X, typename Out, int GROUP>
+hipError_t launch(const W4Args& a, hipStream_t s) {
+  constexpr int RPT = std::is_same_v<X, float> ? 5 : 16;
+  const int tiles = (a.N + 15) / 16, KB = a.K / 128;
+  const int waves = KB < 8 ? KB : 8;
+#define W4(NT, MT)                                                                            \
+  hipLaunchKernelGGL((linear_w4_kernel<X, Out, GROUP, NT, MT>),                               \
+                     dim3((tiles + NT - 1) / NT, (a.M + MT * RPT - 1) / (MT * RPT)),          \
+                     dim3(64 * waves), waves * NT * MT * 1024, s, a)
+  if (a.M <= RPT) {
+    if (tiles < 1024) W4(1, 1);
+    else W4(4, 1);
+  } else {
+    W4(2, 2);
+  }
+#undef W4
+  return hipGetLastError();
+}
+
+template <typename X, typename Out>
+hipError_t launch_group(int group, const W4Args& a, hipStream_t s) {
+  return group == 32   ? launch<X, Out, 32>(a, s)
+         : group == 64 ? launch<X, Out, 64>(a, s)
+                       : launch<X, Out, 128>(a, s);
+}
+
+// One thread per output and group: scale = max |w| / 7 (NaN if a weight of
+// the group is not finite), code = w / scale rounded to nearest, ties to
+// even, + 8.  Outputs past N, up to a whole tile, get scale 0 and code 8.
+template <int GROUP>
+__global__ __launch_bounds__(256) void quantize_w4_kernel(const float* __restrict__ w, int N,
+                                                          int K, uint8_t* __restrict__ codes,
+                                                          float* __restrict__ scales) {
+  const int n = blockIdx.y * 256 + threadIdx.x, grp = blockIdx.x;
+  const int64_t tile = n / 16;
+  if (n >= (N + 15) / 16 * 16) return;
+  const float* p = w + (int64_t)grp * GROUP * N + n;
+  float most = 0.f;
+  bool finite = true;
+  if (n < N) {
+    for (int k = 0; k < GROUP; ++k) {
+      const float v = fabsf(p[(int64_t)k * N]);
+      finite = finite && v <= FLT_MAX;
+      most = fmaxf(most, v);
+    }
+  }
+  const float scale = finite ? most / 7.0f : __builtin_nanf("");
+  scales[(tile * (K / GROUP) + grp) * 16 + n % 16] = scale;
+  for (int o = 0; o < GROUP / 8; ++o) {
+    uint32_t word = 0x88888888u;
+    if (n < N && scale > 0.f) {
+      word = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float q = rintf(p[(int64_t)(8 * o + e) * N] / scale);
+        const uint32_t c = (uint32_t)((int)fminf(fmaxf(q, -8.f), 7.f) + 8);
+        word |= c << (4 * (e / 2 + 4 * (e % 2)));
+      }
+    }
+    const int k = grp * GROUP + 8 * o, lane = k / 8 % 4 * 16 + n % 16;
+    *reinterpret_cast<uint32_t*>(codes + ((tile * (K / 128) + k / 128) * 64 + lane) * 16 +
+                                 k / 32 % 4 * 4) = word;
+  }
+}
+
+acid_status check_w4_shape(int64_t N, int64_t K, int group) {
+  if (N < 1 || K < 1) return set_error(ACID_ERR_INVALID_ARG, "N and K must be >= 1");
+  if (group != 32 && group != 64 && group != 128)
+    return set_error(ACID_ERR_SHAPE, "group %d: 32, 64 or 128", group);
+  if (K % 128 || K > (1 << 22) || N > (1 << 22))
+    return set_error(ACID_ERR_SHAPE, "w4: K %lld must be a multiple of 128, K and N <= 2^22",
+                     (long long)K);
+  return ACID_OK;
+}
+
+}  // namespace
+}  // namespace acid
+
+using namespace acid;
+
+extern "C" {
+
+acid_status acid_quantize_w4(const float* w_dev, int32_t N, int32_t K, int32_t group,
+                             void* codes_dev, float* scales_dev, hipStream_t stream) {
+  ACID_TRY(check_w4_shape(N, K, group));
+  if (!w_dev || !codes_dev || !scales_dev) return set_error(ACID_ERR_INVALID_ARG, "NULL argument");
+  if ((uintptr_t)w_dev % 4 || (uintptr_t)codes_dev % 16 || (uintptr_t)scales_dev % 4)
+    return set_error(ACID_ERR_INVALID_ARG, "codes must be 16-byte aligned, w and scales 4-byte");
+  const int64_t padded = round_up(N, 16), wb = (int64_t)N * K * 4, cb = padded * K / 2,
+                sb = padded * (K / group) * 4;
+  if (bytes_overlap(w_dev, wb, codes_dev, cb) || bytes_overlap(w_dev, wb, scales_dev, sb) ||
+      bytes_overlap(codes_dev, cb, scales_dev, sb))
+    return set_error(ACID_ERR_INVALID_ARG, "w, codes and scales overlap");
+  StreamDevice on;
+  ACID_TRY(on.enter(stream));
+  const dim3 grid((unsigned)(K / group), (unsigned)((padded + 255) / 256));
+#define QW(G) hipLaunchKernelGGL(quantize_w4_kernel<G>, grid, dim3(256), 0, stream, w_dev, N, K, (uint8_t*)codes_dev, scales_dev)
+  if (group == 32) QW(32);
+  else if (group == 64) QW(64);
+  else QW(128);
+#undef QW
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? ACID_OK : check_hip(e, "quantize w4");
+}
+
+acid_status acid_linear_w4(int32_t x_dtype, int64_t M, int32_t N, int32_t K, int32_t group,
+                           const void* x_dev, int64_t x_ld, const void* codes_dev,
+                           const float* scales_dev, const float* bias_dev, int32_t kind,
+                           int32_t out_dtype, void* out_dev, int64_t out_ld, hipStream_t stream) {
+  for (int dt : {x_dtype, out_dtype})
+    if (dt != ACID_F32 && dt != ACID_BF16)
+      return set_error(ACID_ERR_INVALID_ARG, "bad dtype %d", dt);
+  if (kind != ACID_EPI_BIAS && kind != ACID_EPI_BIAS_GELU)
+    return set_error(ACID_ERR_UNSUPPORTED, "w4: epilogue %d is not BIAS or BIAS_GELU", kind);
+  if (M < 0) return set_error(ACID_ERR_INVALID_ARG, "M < 0");
+  ACID_TRY(check_w4_shape(N, K, group));
+  const int64_t xs = x_dtype == ACID_BF16 ? 2 : 4, os = out_dtype == ACID_BF16 ? 2 : 4;
+  if (M > 65536) return set_error(ACID_ERR_SHAPE, "w4: M %lld: at most 65536 rows", (long long)M);
+  if (x_ld < K || x_ld * xs % 16 || x_ld > ((int64_t)1 << 32) || out_ld < N ||
+      out_ld > ((int64_t)1 << 32))
+    return set_error(ACID_ERR_SHAPE,
+                     "w4: x_ld >= K and whole 16 bytes, out_ld >= N, both <= 2^32");
+  if (M == 0) return ACID_OK;
+  if (!x_dev || !codes_dev || !scales_dev || !out_dev)
+    return set_error(ACID_ERR_INVALID_ARG, "NULL argument");
+  if (((uintptr_t)x_dev | (uintptr_t)codes_dev) % 16 || (uintptr_t)out_dev % os ||
+      ((uintptr_t)scales_dev | (uintptr_t)bias_dev) % 4)
+    return set_error(ACID_ERR_INVALID_ARG, "x and codes must be 16-byte aligned, the rest to an element");
+  const int64_t padded = round_up(N, 16);
+  const struct {
+    const void* p;
+    int64_t rows, width, ld;
+  } in[] = {{x_dev, M, K * xs, x_ld * xs},
+            {codes_dev, 1, padded * K / 2, padded * K / 2},
+            {scales_dev, 1, padded * (K / group) * 4, padded * (K / group) * 4},
+            {bias_dev, 1, (int64_t)N * 4, (int64_t)N * 4}};
+  for (const auto& i : in)
+    if (rows_overlap(out_dev, M, N * os, out_ld * os, i.p, i.rows, i.width, i.ld))
+      return set_error(ACID_ERR_INVALID_ARG, "w4: out overlaps an input");
+  StreamDevice on;
+  ACID_TRY(on.enter(stream));
+  const W4Args a = {x_dev, (const uint8_t*)codes_dev, scales_dev, bias_dev, out_dev, x_ld, out_ld,
+                    (int32_t)M, N, K, kind == ACID_EPI_BIAS_GELU};
+  hipError_t e;
+  if (x_dtype == ACID_BF16)
+    e = out_dtype == ACID_BF16 ? launch_group<bf16, bf16>(group, a, stream)
+                               : launch_group<bf16, float>(group, a, stream);
+  else
+    e = out_dtype == ACID_BF16 ? launch_group<float, bf16>(group, a, stream)
+                               : launch_group<float, float>(group, a, stream);
+  return e == hipSuccess ? ACID_OK : check_hip(e, "linear w4");
+}
+
+}  // extern "C"
