@@ -4,28 +4,22 @@
 //   S_t = lambda S_{t-1} + k_t^T v_t,  o_t = scale q_t S_t,  lambda = exp(-slope)
 //
 // S is fp32 [d][d] (rows over k's columns, columns over v's).
+#include <type_traits>
+
 #include "common.h"
 
 namespace acid {
 namespace {
 
-// Where a sequence's or row's vectors lie, in elements.
-struct Strides {
-  int64_t seq, head, token;
-};
-
-struct RecurrentArgs {
+struct StepArgs {
   const void *q, *k, *v;
   void* o;
-  Strides qs, ks, vs, os;
-  int64_t v_col;  // distance of v's columns
+  int64_t q_ld, k_ld, v_ld, o_ld;
   const float* slopes;
-  const int32_t* lengths;  // tokens of each sequence, or null: all
-  const int32_t* slots;    // step: state of each row, or null: its own index
+  const int32_t* slots;  // state of each row, or null: its own index
   const float* state_in;
   float* state_out;
-  int64_t tokens;  // of a sequence; step: rows
-  int64_t n_slots;
+  int64_t rows, n_slots;
   int32_t heads;
   float scale;
 };
@@ -42,57 +36,46 @@ __device__ __forceinline__ int64_t find_slot(const int32_t* __restrict__ slots, 
   return -1;
 }
 
-// The recurrence as it stands, one token after the other.  A workgroup owns
-// 32 columns of one head's state: thread (rg, cg) holds rows rg + 32 i,
-// columns 4 cg .. 4 cg + 3.
-template <typename T, int D, bool STEP>
-__global__ __launch_bounds__(256) void la_recurrent_kernel(RecurrentArgs a) {
+// One token a row.  A workgroup owns 32 columns of one head's state: thread
+// (rg, cg) holds rows rg + 32 i, columns 4 cg .. 4 cg + 3.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void la_step_kernel(StepArgs a) {
   constexpr int R = D / 32;
   __shared__ float part[2][4][32];
   const int cg = threadIdx.x & 7, rg = threadIdx.x >> 3, wave = threadIdx.x >> 6;
   const int slice = blockIdx.x % R;
   const int head = (blockIdx.x / R) % a.heads;
-  const int64_t seq = blockIdx.x / R / a.heads;
+  const int64_t row = blockIdx.x / R / a.heads;
 
-  int64_t slot = seq, t = 0, end = a.tokens;
-  if constexpr (STEP) {
-    t = seq;
-    if (a.slots) {
-      slot = a.slots[seq];
-      if (slot < 0 || slot >= a.n_slots) return;  // padding
-      // rows of one slot are one sequence's successive tokens: the first
-      // row's workgroup takes them all
-      if (find_slot(a.slots, (int32_t)slot, 0, seq) >= 0) return;
-    }
-  } else if (a.lengths) {
-    const int64_t n = a.lengths[seq];
-    end = n < 0 ? 0 : n < end ? n : end;
+  int64_t slot = row;
+  if (a.slots) {
+    slot = a.slots[row];
+    if (slot < 0 || slot >= a.n_slots) return;  // padding
+    // rows of one slot are one sequence's successive tokens: the first row's
+    // workgroup takes them all
+    if (find_slot(a.slots, (int32_t)slot, 0, row) >= 0) return;
   }
-  const T* q = (const T*)a.q + (STEP ? 0 : seq * a.qs.seq) + head * a.qs.head;
-  const T* k = (const T*)a.k + (STEP ? 0 : seq * a.ks.seq) + head * a.ks.head;
-  const T* v = (const T*)a.v + (STEP ? 0 : seq * a.vs.seq) + head * a.vs.head;
-  T* o = (T*)a.o + (STEP ? 0 : seq * a.os.seq) + head * a.os.head;
+  const T* q = (const T*)a.q + head * D;
+  const T* k = (const T*)a.k + head * D;
+  const T* v = (const T*)a.v + head * D + slice * 32 + cg * 4;
+  T* o = (T*)a.o + head * D + slice * 32;
   const int64_t at = (slot * a.heads + head) * (D * D) + slice * 32 + cg * 4;
   const float lambda = expf(-a.slopes[head]);
 
   float4 s[R];
 #pragma unroll
   for (int i = 0; i < R; ++i)
-    s[i] = a.state_in ? *reinterpret_cast<const float4*>(a.state_in + at + (rg + 32 * i) * D)
-                      : make_float4(0.f, 0.f, 0.f, 0.f);
+    s[i] = *reinterpret_cast<const float4*>(a.state_in + at + (rg + 32 * i) * D);
   int parity = 0;
-  while (t >= 0 && t < end) {
-    float4 vt;
-    const T* vp = v + t * a.vs.token + (slice * 32 + cg * 4) * a.v_col;
-    vt.x = (float)vp[0];
-    vt.y = (float)vp[a.v_col];
-    vt.z = (float)vp[2 * a.v_col];
-    vt.w = (float)vp[3 * a.v_col];
+  for (int64_t t = row; t >= 0;
+       t = a.slots ? find_slot(a.slots, (int32_t)slot, t + 1, a.rows) : -1) {
+    const T* vp = v + t * a.v_ld;
+    const float4 vt = make_float4((float)vp[0], (float)vp[1], (float)vp[2], (float)vp[3]);
     float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const float kt = (float)k[t * a.ks.token + rg + 32 * i];
-      const float qt = (float)q[t * a.qs.token + rg + 32 * i];
+      const float kt = (float)k[t * a.k_ld + rg + 32 * i];
+      const float qt = (float)q[t * a.q_ld + rg + 32 * i];
       s[i].x = lambda * s[i].x + kt * vt.x;
       s[i].y = lambda * s[i].y + kt * vt.y;
       s[i].z = lambda * s[i].z + kt * vt.z;
@@ -114,26 +97,18 @@ __global__ __launch_bounds__(256) void la_recurrent_kernel(RecurrentArgs a) {
     if (threadIdx.x < 32) {
       const float sum = (part[parity][0][threadIdx.x] + part[parity][1][threadIdx.x]) +
                         (part[parity][2][threadIdx.x] + part[parity][3][threadIdx.x]);
-      o[t * a.os.token + slice * 32 + threadIdx.x] = (T)(a.scale * sum);
+      o[t * a.o_ld + threadIdx.x] = (T)(a.scale * sum);
     }
     parity ^= 1;
-    if constexpr (STEP)
-      t = a.slots ? find_slot(a.slots, (int32_t)slot, t + 1, end) : -1;
-    else
-      ++t;
   }
-  if (a.state_out) {
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-      *reinterpret_cast<float4*>(a.state_out + at + (rg + 32 * i) * D) = s[i];
-  }
+  for (int i = 0; i < R; ++i)
+    *reinterpret_cast<float4*>(a.state_out + at + (rg + 32 * i) * D) = s[i];
 }
 
-template <bool STEP>
-hipError_t launch_recurrent(int dtype, int d, int64_t seqs, const RecurrentArgs& a,
-                            hipStream_t s) {
-  const dim3 grid((unsigned)(seqs * a.heads * (d / 32)));
-#define LA(T, D) hipLaunchKernelGGL((la_recurrent_kernel<T, D, STEP>), grid, dim3(256), 0, s, a)
+hipError_t launch_step(int dtype, int d, const StepArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.rows * a.heads * (d / 32)));
+#define LA(T, D) hipLaunchKernelGGL((la_step_kernel<T, D>), grid, dim3(256), 0, s, a)
   if (dtype == ACID_BF16) {
     if (d == 64) LA(bf16, 64);
     else LA(bf16, 128);
@@ -142,6 +117,710 @@ hipError_t launch_recurrent(int dtype, int d, int64_t seqs, const RecurrentArgs&
     else LA(float, 128);
   }
 #undef LA
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------- whole sequences
+//
+// In chunks of C = 64 tokens (i, j within a chunk):
+//
+//   O = scale (diag(lambda^(i+1)) Q S + ((Q K^T) (.) lambda^(i-j), j <= i) V)
+//   S' = lambda^C S + sum_j k_j^T (lambda^(C-1-j) v_j)
+//
+// A workgroup of D / 16 waves takes a run of chunks of one head, S in the
+// accumulators of its waves, each of which owns 16 of v's columns: [D][16] a
+// wave, tiles of 16 x 16 whose lane (g, col) holds rows 4 g + i, column col.
+// Two tiles' registers are then eight columns of k, 32 kk + 4 g .. + 3 and
+// 32 kk + 16 + 4 g .. + 3: the operand of Q S as it stands, with no trip through
+// LDS.  V is an operand as it lies in memory (vt's rows), read by its wave
+// alone, so the decay goes onto V and not onto K, which all waves share.  O is
+// formed transposed (rows: v's columns, columns: tokens), so that a lane
+// stores four neighbouring values.
+//
+// LDS holds what the waves share: Q's and K's rows, loaded there directly a
+// chunk ahead, and the masked scores.  K's operand of the outer products lies
+// across those rows; bf16 reads it with the transposing LDS load.
+//
+// Rounding.  A bf16 operand made from fp32 values would cost the output half
+// of its accuracy, so scores and S go into their products as two bf16 parts
+// (relative error 2^-16).  So does the decayed V where S is only read by the
+// chunks that follow; where it is summed to an fp32 state that is returned, or
+// carried to another segment, V goes in as three parts, which is exact.
+constexpr int kChunk = 64;
+constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 64;
+
+template <typename T>
+struct Operand;  // eight values of the contracted index
+template <>
+struct Operand<bf16> {
+  bf16x8 v;
+};
+template <>
+struct Operand<float> {
+  f32x4 a, b;
+};
+
+__device__ __forceinline__ Operand<bf16> load8(const bf16* p) {
+  return {*reinterpret_cast<const bf16x8*>(p)};
+}
+__device__ __forceinline__ Operand<float> load8(const float* p) {
+  return {reinterpret_cast<const f32x4*>(p)[0], reinterpret_cast<const f32x4*>(p)[1]};
+}
+// Values at and after index n become zeros, whatever they were.
+__device__ __forceinline__ void keep_first(Operand<bf16>& x, int n) {
+  const bf16x8 v = x.v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x.v[e] = e < n ? v[e] : (bf16)0.0f;
+}
+__device__ __forceinline__ void keep_first(Operand<float>& x, int n) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x.a[e] = e < n ? x.a[e] : 0.f;
+    x.b[e] = e + 4 < n ? x.b[e] : 0.f;
+  }
+}
+__device__ __forceinline__ f32x4 mma(const Operand<bf16>& a, const Operand<bf16>& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+// The fp32 instruction contracts one value a lane, so element e of both
+// operands makes one product: the same 32 indices in another order.
+__device__ __forceinline__ f32x4 mma(const Operand<float>& a, const Operand<float>& b, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.a[e], b.a[e], c, 0, 0, 0);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.b[e], b.b[e], c, 0, 0, 0);
+  return c;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A value that is the same in every lane, kept in a scalar register.
+__device__ __forceinline__ float uniform(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+
+// log2(e) slope: the decay over n tokens is exp2(-rate n).  Capped, so that an
+// infinite slope still gives 1 over no tokens.
+__device__ __forceinline__ float decay_rate(float slope) {
+  const float c = slope * 1.44269504088896341f;
+  return uniform(c > 1e30f ? 1e30f : c);
+}
+
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+__device__ __forceinline__ uint64_t uniform_ptr(const void* p) {
+  const uint64_t v = (uint64_t)(uintptr_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return ((uint64_t)hi << 32) | lo;
+}
+// Lane l copies 16 bytes at base + off_bytes(l) to LDS bytes [lds + 16 l, +16).
+// base and lds are wave-uniform; the compiler does not see the load, which
+// barrier_all() waits for.
+__device__ __forceinline__ void dma16(uint64_t base, uint32_t off_bytes, uint32_t lds_byte) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(off_bytes), "s"(base), "s"(lds_byte)
+      : "memory");
+}
+__device__ __forceinline__ void barrier_all() {  // loads into LDS included
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+__device__ __forceinline__ void barrier_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// 64 rows of W values in LDS, in 16-byte chunks: chunk c of row r is at slot
+// c ^ swizzle(r).  With 64 banks of four bytes, all of these hit each bank
+// equally often: half chunks of 16 neighbouring rows (split_operand); two
+// neighbouring chunks of rows 8 g + 0 .. 3 (bf16 across the rows) or four of rows
+// 8 g (fp32 across the rows); whole chunks of 16 rows of scores (row_operand; of
+// bf16 rows of K and Q they would take two turns).
+//
+// Rows are a power of two long and the swizzle is linear in r's bits, so
+// at(r ^ r1, x ^ x1) == at(r, x) ^ at(r1, x1): a lane keeps one address and
+// every place it reads is that address with a constant's bits flipped (or, for
+// rows that the swizzle does not see, at a constant distance).
+template <typename T, int W, bool SCORES = false>
+struct Rows {
+  static constexpr int BYTES = W * (int)sizeof(T), CHUNK = 16 / (int)sizeof(T);
+  static constexpr int TOTAL = kChunk * BYTES;
+  static constexpr int swizzle(int r) {
+    const int b0 = r & 1, b1 = r >> 1 & 1, b2 = r >> 2 & 1, b3 = r >> 3 & 1, b4 = r >> 4 & 1;
+    return sizeof(T) == 4 ? b0 | b1 << 1 | b3 << 2 | (b2 ^ b4) << 3
+           : W == kChunk && SCORES ? b1 | b2 << 1 | b3 << 2
+           : BYTES == 256 ? b2 | b0 << 1 | b1 << 2 | b3 << 3
+                          : b2 | b1 << 1 | b3 << 2;  // 128 bytes: odd rows lie in the other banks
+  }
+  static constexpr uint32_t at(int r, int x) {  // bytes
+    return (uint32_t)(r * BYTES + ((x / CHUNK ^ swizzle(r)) * 16) + x % CHUNK * (int)sizeof(T));
+  }
+  // what a step of 16 t rows, 16 t BYTES apart, flips besides
+  static constexpr uint32_t tile_bits(int t) { return (uint32_t)(swizzle(16 * t) * 16); }
+};
+
+template <typename V>
+__device__ __forceinline__ V lds_read(uint32_t at) {
+  return *(const __attribute__((address_space(3))) V*)at;
+}
+template <typename V>
+__device__ __forceinline__ void lds_write(uint32_t at, V v) {
+  *(__attribute__((address_space(3))) V*)at = v;
+}
+// Keeps the addresses made from x out of registers across a loop.
+__device__ __forceinline__ uint32_t afresh(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The tile of rows c0 .. c0 + n - 1 (base: row c0) into LDS, rows past it as
+// copies of the last one: sizeof(T) instructions of each of W / 16 waves.
+template <typename T, int W>
+__device__ __forceinline__ void load_rows(uint64_t base, int n, uint32_t lds, int wave, int lane) {
+  typedef Rows<T, W> R;
+  constexpr int SLOTS = W / R::CHUNK;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T); ++i) {
+    const int piece = (wave * (int)sizeof(T) + i) * 64 + lane;  // 16-byte piece of the tile
+    const int r = piece / SLOTS, c = piece % SLOTS ^ R::swizzle(r);
+    const int row = r < n ? r : n - 1;
+    dma16(base, (uint32_t)(row * R::BYTES + c * 16), lds + (wave * (int)sizeof(T) + i) * 1024);
+  }
+}
+
+// Operand along a row of scores: eight values from column 8 g (base: there) +
+// X, X a multiple of 32.  `off`: a constant distance.
+__device__ __forceinline__ Operand<bf16> score_operand(uint32_t base, int X, int off, bf16) {
+  return {lds_read<bf16x8>((base ^ Rows<bf16, kChunk, true>::at(0, X)) + off)};
+}
+__device__ __forceinline__ Operand<float> score_operand(uint32_t base, int X, int off, float) {
+  typedef Rows<float, kChunk, true> P;
+  return {lds_read<f32x4>((base ^ P::at(0, X)) + off),
+          lds_read<f32x4>((base ^ P::at(0, X + 4)) + off)};
+}
+// Operand along a row of Q or K: four values from column 4 g (base: there) + X
+// and four from 16 further.
+template <int W>
+__device__ __forceinline__ Operand<bf16> split_operand(uint32_t base, int X, int off, bf16) {
+  const bf16x4 a = lds_read<bf16x4>((base ^ Rows<bf16, W>::at(0, X)) + off);
+  const bf16x4 b = lds_read<bf16x4>((base ^ Rows<bf16, W>::at(0, X + 16)) + off);
+  return {__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
+}
+template <int W>
+__device__ __forceinline__ Operand<float> split_operand(uint32_t base, int X, int off, float) {
+  return {lds_read<f32x4>((base ^ Rows<float, W>::at(0, X)) + off),
+          lds_read<f32x4>((base ^ Rows<float, W>::at(0, X + 16)) + off)};
+}
+// Operand across the rows: column X + lane % 16 of rows 8 g .. 8 g + 7, X a
+// multiple of 16.  The transposing load hands the 16 lanes of a group the 16
+// columns of four rows of which each lane has addressed four values.
+template <typename T, int W>
+__device__ __forceinline__ uint32_t column_base(int lane) {
+  const int l = lane & 15, g = lane >> 4;
+  return sizeof(T) == 2 ? Rows<T, W>::at(8 * g + (l >> 2), 4 * (l & 3)) : Rows<T, W>::at(8 * g, l);
+}
+template <int W>
+__device__ __forceinline__ Operand<bf16> column_operand(uint32_t base, int X, int off, bf16) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s16x4* Lds;
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)((base ^ Rows<bf16, W>::at(0, X)) + off));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)((base ^ Rows<bf16, W>::at(4, X)) + off));
+  return {__builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7))};
+}
+template <int W>
+__device__ __forceinline__ Operand<float> column_operand(uint32_t base, int X, int off, float) {
+  Operand<float> out;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    out.a[e] = lds_read<float>((base ^ Rows<float, W>::at(e, X)) + off);
+    out.b[e] = lds_read<float>((base ^ Rows<float, W>::at(e + 4, X)) + off);
+  }
+  return out;
+}
+
+template <int D>
+struct State {
+  f32x4 t[D / 16];
+};
+
+// A wave's 16 columns of V for 64 tokens, as they are an operand: vt's rows,
+// tokens 32 ks + 8 g .. + 7 in lane g.
+template <typename T>
+struct ValueTile {
+  Operand<T> v[2];
+  __device__ __forceinline__ void load(const T* vt, int64_t vt_ld, int64_t c0, int64_t len,
+                                       int wave, int lane) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const int64_t t = c0 + 32 * ks + 8 * (lane >> 4);
+      v[ks] = load8(vt + (wave * 16 + (lane & 15)) * vt_ld + (t < len ? t : 0));
+    }
+  }
+  // tokens from n on become zeros
+  __device__ __forceinline__ void mask(int n, int lane) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) keep_first(v[ks], n - 32 * ks - 8 * (lane >> 4));
+  }
+};
+
+// The decays over 7, 6, .. 0 tokens, the same in every lane.
+struct Powers {
+  float p[8];
+  __device__ __forceinline__ explicit Powers(float rate) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      p[e] = uniform(exp2_fast(-rate * (float)(7 - e)));
+  }
+};
+
+// x - hi's value i, exactly, where hi[i] is x cut or rounded to bf16.
+template <int I>
+__device__ __forceinline__ float rest(float x, bf16x2 hi) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, hi);
+  return x - __uint_as_float(I ? u & 0xffff0000u : u << 16);
+}
+__device__ __forceinline__ bf16x2 cut(float x0, float x1) {
+  return __builtin_bit_cast(
+      bf16x2, __builtin_amdgcn_perm(__float_as_uint(x1), __float_as_uint(x0), 0x07060302u));
+}
+
+// V times the tokens' decays, as operands whose sum it is: each product cut
+// to its first eight significant bits, the next eight, the rest.
+template <int PARTS>
+__device__ __forceinline__ void decayed(const Operand<bf16>& v, const float (&w)[8],
+                                        Operand<bf16> (&out)[PARTS]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x0 = (float)v.v[2 * i] * w[2 * i], x1 = (float)v.v[2 * i + 1] * w[2 * i + 1];
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+      const bf16x2 c = cut(x0, x1);
+      out[p].v[2 * i] = c[0];
+      out[p].v[2 * i + 1] = c[1];
+      if (p + 1 < PARTS) {
+        x0 = rest<0>(x0, c);
+        x1 = rest<1>(x1, c);
+      }
+    }
+  }
+}
+template <int PARTS>
+__device__ __forceinline__ void decayed(const Operand<float>& v, const float (&w)[8],
+                                        Operand<float> (&out)[PARTS]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    out[0].a[e] = v.a[e] * w[e];
+    out[0].b[e] = v.b[e] * w[4 + e];
+  }
+}
+
+// S += K^T (decayed V) over 64 tokens; token t decays over last - t, last >= 63
+// if WHOLE.  columns: K's tile plus column_base().
+template <typename T, int D, int PARTS, bool WHOLE>
+__device__ __forceinline__ void add_outer(State<D>& s, uint32_t columns, const ValueTile<T>& v,
+                                          float rate, const Powers& pw, int last, int lane) {
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    const int far = last - 32 * ks - 8 * (lane >> 4);  // of the lane's first token
+    float w[8];
+    if constexpr (WHOLE) {
+      const float first = exp2_fast(-rate * (float)(far - 7));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = first * pw.p[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = exp2_fast(-rate * (float)(far > e ? far - e : 0));
+    }
+    Operand<T> b[PARTS];
+    decayed(v.v[ks], w, b);
+#pragma unroll
+    for (int kt = 0; kt < D / 16; ++kt) {
+      const Operand<T> a = column_operand<D>(columns, 16 * kt, 32 * ks * Rows<T, D>::BYTES, T());
+#pragma unroll
+      for (int p = PARTS - 1; p >= 0; --p) s.t[kt] = mma(a, b[p], s.t[kt]);
+      if (kt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+}
+
+struct ChunkArgs {
+  const void *q, *k, *vt;
+  void* o;
+  int64_t vt_ld;
+  const float* slopes;
+  const int32_t* lengths;
+  const float* state_in;
+  float* state_out;
+  float* slots;  // [n_seq][heads][segments][D][D], or null: one segment
+  int64_t tokens;
+  int32_t heads, segments, segment;  // segment: tokens of one, a multiple of 64
+  int32_t scanned;
+  float scale;
+};
+
+__device__ __forceinline__ int64_t length_of(const int32_t* lengths, int64_t seq, int64_t tokens) {
+  if (!lengths) return tokens;
+  const int64_t n = lengths[seq];
+  return n < 0 ? 0 : n < tokens ? n : tokens;
+}
+
+// A wave's share of a state in the workspace lies tile by tile as its lanes
+// hold it; a caller's is [D][D].  f(tile, workspace index, row, column).
+template <int D, typename F>
+__device__ __forceinline__ void for_state(State<D>& s, F&& f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int kt = 0; kt < D / 16; ++kt)
+    f(s.t[kt], (wave * (D / 16) + kt) * 256 + lane * 4, 16 * kt + 4 * (lane >> 4),
+      wave * 16 + (lane & 15));
+}
+template <int D>
+__device__ __forceinline__ void read_state(State<D>& s, const float* p) {
+  for_state(s, [&](f32x4& t, int, int row, int col) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = p[(row + i) * D + col];
+  });
+}
+template <int D>
+__device__ __forceinline__ void write_state(State<D>& s, float* p) {
+  for_state(s, [&](f32x4& t, int, int row, int col) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[(row + i) * D + col] = t[i];
+  });
+}
+
+// Where there are too few heads to fill the chip, a sequence is cut into
+// segments.  This kernel leaves in slot j + 1 what segment j adds to the state
+// (segment 0: what it makes of state_in), for each segment that another
+// follows, and in slot 0 state_in itself, which the outputs' kernel may
+// overwrite in place.
+template <typename T, int D>
+__global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_state_kernel(ChunkArgs a) {
+  typedef Rows<T, D> R;
+  __shared__ __align__(1024) unsigned char rows[2 * R::TOTAL];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int seg = blockIdx.x % (a.segments - 1);
+  const int64_t hs = blockIdx.x / (a.segments - 1);  // sequence and head
+  const int head = hs % a.heads;
+  const int64_t len = length_of(a.lengths, hs / a.heads, a.tokens);
+  const int64_t begin = (int64_t)seg * a.segment, end = begin + a.segment;
+  float* slot = a.slots + (hs * a.segments + seg) * (D * D);
+  State<D> s;
+  if (seg == 0 && a.state_in && len > 0) {
+    read_state(s, a.state_in + hs * (D * D));
+    for_state(s, [&](f32x4& t, int at, int, int) { *reinterpret_cast<f32x4*>(slot + at) = t; });
+  }
+  if (end >= len) return;  // no segment follows
+  constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
+  const float rate = decay_rate(a.slopes[head]);
+  const Powers pw(rate);
+  if (seg == 0 && a.state_in) {
+    const float w = (float)exp(-(double)a.slopes[head] * a.segment);
+    for_state(s, [&](f32x4& t, int, int, int) { t *= w; });
+  } else {
+    for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{0.f, 0.f, 0.f, 0.f}; });
+  }
+  const T* k = (const T*)a.k + hs * a.tokens * D;
+  const T* vt = (const T*)a.vt + hs * D * a.vt_ld;
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void_t*)rows;
+  ValueTile<T> v, v_next;
+  load_rows<T, D>(uniform_ptr(k + begin * D), kChunk, lds, wave, lane);
+  v.load(vt, a.vt_ld, begin, len, wave, lane);
+  uint32_t buf = lds, next = lds + R::TOTAL;
+  for (int64_t c0 = begin; c0 < end; c0 += kChunk) {
+    barrier_all();
+    if (c0 + kChunk < end) {
+      load_rows<T, D>(uniform_ptr(k + (c0 + kChunk) * D), kChunk, next, wave, lane);
+      v_next.load(vt, a.vt_ld, c0 + kChunk, len, wave, lane);
+    }
+    add_outer<T, D, PARTS, true>(s, afresh(buf + column_base<T, D>(lane)), v, rate, pw,
+                                 (int)(end - 1 - c0), lane);
+    v = v_next;
+    const uint32_t t = buf;
+    buf = next;
+    next = t;
+  }
+  for_state(s, [&](f32x4& t, int at, int, int) {
+    *reinterpret_cast<f32x4*>(slot + D * D + at) = t;
+  });
+}
+
+// Slot j becomes the state before segment j: x_j = lambda^segment x_{j-1} +
+// slot j, in place, the chain in fp64 (a rounded factor would add up over the
+// segments).
+template <int D>
+__global__ __launch_bounds__(256) void la_scan_kernel(ChunkArgs a) {
+  constexpr int GROUPS = D * D / 512;
+  const int64_t hs = blockIdx.x / GROUPS;
+  const int64_t len = length_of(a.lengths, hs / a.heads, a.tokens);
+  const int last = len > 0 ? (int)((len - 1) / a.segment) : 0;  // the sequence's last segment
+  const double lambda = exp(-(double)a.slopes[hs % a.heads] * a.segment);
+  float2* p = reinterpret_cast<float2*>(a.slots + hs * a.segments * (D * D)) +
+              (blockIdx.x % GROUPS) * 256 + threadIdx.x;
+  constexpr int STEP = D * D / 2;
+  double x = 0.0, y = 0.0;
+  int j = 1;
+  for (; j + 7 <= last; j += 8) {
+    float2 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p[(int64_t)(j + i) * STEP];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x = lambda * x + v[i].x;
+      y = lambda * y + v[i].y;
+      p[(int64_t)(j + i) * STEP] = make_float2((float)x, (float)y);
+    }
+  }
+  for (; j <= last; ++j) {
+    const float2 v = p[(int64_t)j * STEP];
+    x = lambda * x + v.x;
+    y = lambda * y + v.y;
+    p[(int64_t)j * STEP] = make_float2((float)x, (float)y);
+  }
+}
+
+// S as the two-part (fp32: whole) operand of Q S: columns 32 kk + 4 g .. + 3 and
+// 32 kk + 16 + 4 g .. + 3 of k in lane g.
+template <int D>
+__device__ __forceinline__ void state_operand(const State<D>& s, int kk, Operand<bf16> (&out)[2]) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const f32x4 t = s.t[2 * kk + (e >> 2)];
+    const bf16x2 hi = {(bf16)t[e & 3], (bf16)t[(e & 3) + 1]};
+    out[0].v[e] = hi[0];
+    out[0].v[e + 1] = hi[1];
+    out[1].v[e] = (bf16)rest<0>(t[e & 3], hi);
+    out[1].v[e + 1] = (bf16)rest<1>(t[(e & 3) + 1], hi);
+  }
+}
+template <int D>
+__device__ __forceinline__ void state_operand(const State<D>& s, int kk, Operand<float> (&out)[1]) {
+  out[0] = {s.t[2 * kk], s.t[2 * kk + 1]};
+}
+
+// Four neighbouring scores of one token into LDS.
+__device__ __forceinline__ void store_scores(uint32_t at, int part_stride, f32x4 v, bf16) {
+  const bf16x2 h0 = {(bf16)v[0], (bf16)v[1]}, h1 = {(bf16)v[2], (bf16)v[3]};
+  const bf16x4 lo = {(bf16)rest<0>(v[0], h0), (bf16)rest<1>(v[1], h0), (bf16)rest<0>(v[2], h1),
+                     (bf16)rest<1>(v[3], h1)};
+  lds_write(at, (bf16x4)__builtin_shufflevector(h0, h1, 0, 1, 2, 3));
+  lds_write(at + part_stride, lo);
+}
+__device__ __forceinline__ void store_scores(uint32_t at, int, f32x4 v, float) {
+  lds_write(at, v);
+}
+
+__device__ __forceinline__ void store_out(bf16* p, f32x4 v) {
+  bf16x4 b;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = (bf16)v[i];
+  *reinterpret_cast<bf16x4*>(p) = b;
+}
+__device__ __forceinline__ void store_out(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
+
+// The outputs of one segment, from the state before it.  LAST: the sequence's
+// last segment, which leaves the final state.
+template <typename T, int D, bool LAST>
+__device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* rows, int seg,
+                                          int64_t hs, int64_t len, int64_t begin, int64_t end) {
+  constexpr int TWO = sizeof(T) == 2 ? 2 : 1;  // parts of scores and of S
+  constexpr int PARTS = sizeof(T) == 2 ? (LAST ? 3 : 2) : 1;  // LAST: S is an output, in fp32
+  typedef Rows<T, D> R;
+  typedef Rows<T, kChunk, true> P;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = hs % a.heads;
+  const int64_t seq = hs / a.heads;
+  const float slope = a.slopes[head], rate = decay_rate(slope);
+
+  const T* q = (const T*)a.q + hs * a.tokens * D;
+  const T* k = (const T*)a.k + hs * a.tokens * D;
+  const T* vt = (const T*)a.vt + hs * D * a.vt_ld;
+  T* o = (T*)a.o + (seq * a.tokens * a.heads + head) * D + wave * 16;
+  // lambda^64 in two parts: a rounded factor would add up over the chunks
+  const double whole = exp(-(double)slope * kChunk);
+  const Powers pw(rate);
+  const float whole_hi = uniform((float)whole);
+  const float whole_lo = uniform((float)(whole - (double)whole_hi));
+  uint32_t buf = (uint32_t)(uintptr_t)(lds_void_t*)rows, next = buf + 2 * R::TOTAL;
+  const uint32_t scores = buf + 4 * R::TOTAL;
+  ValueTile<T> v, v_next;
+  auto load = [&](int64_t c0, uint32_t to, ValueTile<T>& values, int lane) {
+    const int n = end - c0 < kChunk ? (int)(end - c0) : kChunk;
+    load_rows<T, D>(uniform_ptr(q + c0 * D), n, to, wave, lane);
+    load_rows<T, D>(uniform_ptr(k + c0 * D), n, to + R::TOTAL, wave, lane);
+    values.load(vt, a.vt_ld, c0, len, wave, lane);
+  };
+  if (begin < end) load(begin, buf, v, threadIdx.x & 63);
+
+  State<D> s;
+  if (seg == 0) {
+    if (!a.state_in)
+      for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{0.f, 0.f, 0.f, 0.f}; });
+    else if (a.slots && len > 0)
+      for_state(s, [&](f32x4& t, int at, int, int) {
+        t = *reinterpret_cast<const f32x4*>(a.slots + hs * a.segments * (D * D) + at);
+      });
+    else
+      read_state(s, a.state_in + hs * (D * D));
+  } else {
+    const float* slot = a.slots + (hs * a.segments + seg) * (D * D);
+    for_state(s, [&](f32x4& t, int at, int, int) {
+      t = *reinterpret_cast<const f32x4*>(slot + at);
+    });
+    if (!a.scanned)  // the segments before the last one, each with its decay
+      for (int j = 1; j < seg; ++j) {
+        const float w = exp2_fast(-rate * (float)((seg - j) * a.segment));
+        for_state(s, [&](f32x4& t, int at, int, int) {
+          t += w * *reinterpret_cast<const f32x4*>(slot - (int64_t)(seg - j) * (D * D) + at);
+        });
+      }
+  }
+  // the scores' tiles of this wave: tokens 16 tq .., keys 16 st .., st from
+  // st0 to st1; the tile beside an even diagonal one is written too, as zeros
+  const int tq = D == 128 ? wave >> 1 : wave;
+  const int st0 = D == 128 ? (tq < 2 ? wave & 1 : 2 * (wave & 1)) : 0;
+  const int st1 = D == 128 ? (tq < 2 ? st0 : st0 + 1) : tq | 1;
+
+  int64_t c0 = begin;
+  // One chunk of n tokens: 64, or (WHOLE false) a sequence's last ones.
+  auto chunk = [&](auto whole_chunk, int n, bool update) {
+    constexpr bool WHOLE = decltype(whole_chunk)::value;
+    // made afresh in each chunk: what follows from it is more than registers hold
+    const int lane = (int)afresh(threadIdx.x & 63), col = lane & 15, g = lane >> 4;
+    barrier_all();
+    if (c0 + kChunk < end) load(c0 + kChunk, next, v_next, lane);
+    if (!WHOLE) v.mask(n, lane);
+
+    const uint32_t along = afresh(buf + R::at(col, 4 * g));
+    for (int st = st0; st <= st1; ++st) {
+      f32x4 p = {0.f, 0.f, 0.f, 0.f};
+      if (st <= tq) {
+        const uint32_t k_at = (along ^ R::tile_bits(st)) + R::TOTAL + 16 * st * R::BYTES;
+        const uint32_t q_at = (along ^ R::tile_bits(tq)) + 16 * tq * R::BYTES;
+#pragma unroll
+        for (int kk = 0; kk < D / 32; ++kk)
+          p = mma(split_operand<D>(k_at, 32 * kk, 0, T()), split_operand<D>(q_at, 32 * kk, 0, T()), p);
+      }
+      const int far = 16 * (tq - st) + col - 4 * g;  // from the lane's first key
+      if (st < tq) {
+        const float w = a.scale * exp2_fast(-rate * (float)(far - 3));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] *= w * pw.p[4 + i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          p[i] = far >= i ? p[i] * (a.scale * exp2_fast(-rate * (float)(far - i))) : 0.f;
+      }
+      store_scores(scores + P::at(16 * tq + col, 16 * st + 4 * g), P::TOTAL, p, T());
+    }
+    f32x4 out[4];
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt) out[tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) {
+      Operand<T> sf[TWO];
+      state_operand(s, kk, sf);
+#pragma unroll
+      for (int tt = 0; tt < 4; ++tt) {
+        const Operand<T> qf = split_operand<D>(along ^ R::tile_bits(tt), 32 * kk, 16 * tt * R::BYTES, T());
+#pragma unroll
+        for (int p = TWO - 1; p >= 0; --p) out[tt] = mma(sf[p], qf, out[tt]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+      out[tt] *= a.scale * exp2_fast(-rate * (float)(16 * tt + col + 1));
+    barrier_lds();
+
+    const uint32_t weights = afresh(scores + P::at(col, 8 * g));
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+      for (int ks = 0; ks <= tt / 2; ++ks)
+#pragma unroll
+        for (int p = TWO - 1; p >= 0; --p)
+          out[tt] = mma(v.v[ks],
+                        score_operand(weights ^ P::tile_bits(tt), 32 * ks,
+                                            16 * tt * P::BYTES + p * P::TOTAL, T()),
+                        out[tt]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int tt = 0; tt < 4; ++tt) {
+      const int64_t t = c0 + 16 * tt + col;
+      if (WHOLE || t < end) store_out(o + t * a.heads * D + 4 * g, out[tt]);
+    }
+    if (update) {
+      if constexpr (WHOLE)
+        for_state(s, [&](f32x4& t, int, int, int) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) t[i] = fmaf(t[i], whole_hi, t[i] * whole_lo);
+        });
+      else {
+        const float w = exp2_fast(-rate * (float)n);
+        for_state(s, [&](f32x4& t, int, int, int) { t *= w; });
+      }
+      add_outer<T, D, PARTS, WHOLE>(s, afresh(buf + R::TOTAL + column_base<T, D>(lane)), v, rate,
+                                    pw, n - 1, lane);
+    }
+    v = v_next;
+    const uint32_t t = buf;
+    buf = next;
+    next = t;
+    c0 += kChunk;
+  };
+  while (c0 + kChunk <= end)
+    chunk(std::true_type(), kChunk, (LAST && a.state_out) || c0 + kChunk < end);
+  if constexpr (LAST) {
+    if (c0 < end) chunk(std::false_type(), (int)(end - c0), a.state_out != nullptr);
+    if (a.state_out) write_state(s, a.state_out + hs * (D * D));
+  }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_chunk_kernel(ChunkArgs a) {
+  // LDS: Q's and K's rows of one chunk, of the next one, the scores
+  __shared__ __align__(1024) unsigned char rows[4 * Rows<T, D>::TOTAL +
+                                                (sizeof(T) == 2 ? 2 : 1) * Rows<T, kChunk>::TOTAL];
+  const int seg = blockIdx.x % a.segments;
+  const int64_t hs = blockIdx.x / a.segments;
+  const int64_t len = length_of(a.lengths, hs / a.heads, a.tokens);
+  const int64_t begin = (int64_t)seg * a.segment, end = begin + a.segment;
+  if (end < len)
+    chunks_of<T, D, false>(a, rows, seg, hs, len, begin, end);
+  else if (seg == 0 || begin < len)
+    chunks_of<T, D, true>(a, rows, seg, hs, len, begin, len);
+}
+
+// Tokens of a segment, a multiple of 64, and how many there are.  One segment
+// a head once the heads alone give every CU its two workgroups; else as many
+// as fill them in one round.
+struct Segments {
+  int64_t tokens, count;
+};
+Segments segments_of(int64_t heads, int64_t L) {
+  const int64_t chunks = (L + kChunk - 1) / kChunk, slots = 2 * 256;
+  int64_t most = heads > 0 ? slots / heads : 1;
+  if (most < 1) most = 1;
+  const int64_t per = chunks > most ? (chunks + most - 1) / most : 1;
+  if (chunks <= 1 || most == 1) return {chunks * kChunk, 1};
+  return {per * kChunk, (chunks + per - 1) / per};
+}
+
+template <typename T, int D>
+hipError_t launch_chunks(const ChunkArgs& a, int64_t heads, hipStream_t s) {
+  if (a.segments > 1) {
+    hipLaunchKernelGGL((la_state_kernel<T, D>), dim3((unsigned)(heads * (a.segments - 1))),
+                       dim3(4 * D), 0, s, a);
+    if (a.scanned)
+      hipLaunchKernelGGL((la_scan_kernel<D>), dim3((unsigned)(heads * (D * D / 512))), dim3(256),
+                         0, s, a);
+  }
+  hipLaunchKernelGGL((la_chunk_kernel<T, D>), dim3((unsigned)(heads * a.segments)), dim3(4 * D), 0,
+                     s, a);
   return hipGetLastError();
 }
 
@@ -167,8 +846,12 @@ extern "C" {
 
 size_t acid_linear_attention_workspace_bytes(int64_t n_seq, int32_t n_heads, int64_t seq_len,
                                              int32_t head_dim) {
-  if (check_heads(ACID_BF16, n_seq, n_heads, head_dim) != ACID_OK || seq_len < 0) return 0;
-  return 0;
+  if (check_heads(ACID_BF16, n_seq, n_heads, head_dim) != ACID_OK || seq_len < 0 ||
+      seq_len > kMaxTokens)
+    return 0;
+  const int64_t heads = n_seq * n_heads;
+  const Segments seg = segments_of(heads, seq_len);
+  return seg.count > 1 ? (size_t)(seg.count * heads * head_dim * head_dim * 4) : 0;
 }
 
 acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads, int64_t seq_len,
@@ -180,7 +863,7 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
                                   hipStream_t stream) {
   ACID_TRY(check_heads(dtype, n_seq, n_heads, head_dim));
   if (seq_len < 0) return set_error(ACID_ERR_INVALID_ARG, "seq_len < 0");
-  if (seq_len > ((int64_t)1 << 31) - 64)
+  if (seq_len > kMaxTokens)
     return set_error(ACID_ERR_SHAPE, "seq_len %lld: below 2^31 - 63", (long long)seq_len);
   if (vt_ld < round_up(seq_len, 8) || vt_ld % 8 || vt_ld > ((int64_t)1 << 31))
     return set_error(ACID_ERR_SHAPE,
@@ -208,27 +891,32 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
   if (state_in_dev != state_out_dev &&
       bytes_overlap(state_in_dev, states, state_out_dev, states))
     return set_error(ACID_ERR_INVALID_ARG, "state_in and state_out: one buffer or apart");
-  (void)workspace_bytes;
+  const Segments seg = segments_of(heads, seq_len);
+  if (seg.count > 1) {
+    const int64_t need = seg.count * states;
+    if ((int64_t)workspace_bytes < need || !workspace_dev)
+      return set_error(ACID_ERR_SHAPE, "workspace of %lld bytes, %lld needed",
+                       (long long)(workspace_dev ? workspace_bytes : 0), (long long)need);
+    for (const void* p : {q_dev, k_dev, (const void*)o_dev})
+      if (bytes_overlap(workspace_dev, need, p, qkv))
+        return set_error(ACID_ERR_INVALID_ARG, "the workspace overlaps q, k or o");
+    if (bytes_overlap(workspace_dev, need, vt_dev, vtb) ||
+        bytes_overlap(workspace_dev, need, state_in_dev, states) ||
+        bytes_overlap(workspace_dev, need, state_out_dev, states))
+      return set_error(ACID_ERR_INVALID_ARG, "the workspace overlaps vt or a state");
+  }
   StreamDevice on;
   ACID_TRY(on.enter(stream));
-  RecurrentArgs a = {};
-  a.q = q_dev;
-  a.k = k_dev;
-  a.v = vt_dev;
-  a.o = o_dev;
-  const int64_t d = head_dim;
-  a.qs = a.ks = {n_heads * seq_len * d, seq_len * d, d};
-  a.vs = {n_heads * d * vt_ld, d * vt_ld, 1};
-  a.v_col = vt_ld;
-  a.os = {seq_len * n_heads * d, d, n_heads * d};
-  a.slopes = slopes_dev;
-  a.lengths = lengths_dev;
-  a.state_in = state_in_dev;
-  a.state_out = state_out_dev;
-  a.tokens = seq_len;
-  a.heads = n_heads;
-  a.scale = scale;
-  const hipError_t e = launch_recurrent<false>(dtype, head_dim, n_seq, a, stream);
+  const ChunkArgs a = {q_dev, k_dev, vt_dev, o_dev, vt_ld, slopes_dev, lengths_dev, state_in_dev,
+                       state_out_dev, seg.count > 1 ? (float*)workspace_dev : nullptr, seq_len,
+                       n_heads, (int32_t)seg.count, (int32_t)seg.tokens, seg.count > 8, scale};
+  hipError_t e;
+  if (dtype == ACID_BF16)
+    e = head_dim == 64 ? launch_chunks<bf16, 64>(a, heads, stream)
+                       : launch_chunks<bf16, 128>(a, heads, stream);
+  else
+    e = head_dim == 64 ? launch_chunks<float, 64>(a, heads, stream)
+                       : launch_chunks<float, 128>(a, heads, stream);
   return e == hipSuccess ? ACID_OK : check_hip(e, "linear attention");
 }
 
@@ -275,25 +963,9 @@ acid_status acid_linear_attention_step(int32_t dtype, int64_t n_rows, int32_t n_
     return set_error(ACID_ERR_INVALID_ARG, "state_in and state_out: one buffer or apart");
   StreamDevice on;
   ACID_TRY(on.enter(stream));
-  RecurrentArgs a = {};
-  a.q = q_dev;
-  a.k = k_dev;
-  a.v = v_dev;
-  a.o = o_dev;
-  a.qs = {0, head_dim, q_ld};
-  a.ks = {0, head_dim, k_ld};
-  a.vs = {0, head_dim, v_ld};
-  a.os = {0, head_dim, o_ld};
-  a.v_col = 1;
-  a.slopes = slopes_dev;
-  a.slots = slots_dev;
-  a.n_slots = n_slots;
-  a.state_in = state_in_dev;
-  a.state_out = state_out_dev;
-  a.tokens = n_rows;
-  a.heads = n_heads;
-  a.scale = scale;
-  const hipError_t e = launch_recurrent<true>(dtype, head_dim, n_rows, a, stream);
+  const StepArgs a = {q_dev, k_dev, v_dev, o_dev, q_ld, k_ld, v_ld, o_ld, slopes_dev, slots_dev,
+                      state_in_dev, state_out_dev, n_rows, n_slots, n_heads, scale};
+  const hipError_t e = launch_step(dtype, head_dim, a, stream);
   return e == hipSuccess ? ACID_OK : check_hip(e, "linear attention step");
 }
 
