@@ -227,7 +227,8 @@ __device__ __forceinline__ void dma16(uint64_t base, uint32_t off_bytes, uint32_
       : "memory");
 }
 __device__ __forceinline__ void barrier_all() {  // loads into LDS included
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0);
+  asm volatile("s_barrier" ::: "memory");
 }
 __device__ __forceinline__ void barrier_lds() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -263,7 +264,7 @@ struct Rows {
 };
 
 template <typename V>
-__device__ __forceinline__ V lds_read(uint32_t at) {
+__device__ __forceinline__ std::remove_volatile_t<V> lds_read(uint32_t at) {
   return *(const __attribute__((address_space(3))) V*)at;
 }
 template <typename V>
@@ -303,10 +304,11 @@ __device__ __forceinline__ Operand<float> score_operand(uint32_t base, int X, in
 }
 // Operand along a row of Q or K: four values from column 4 g (base: there) + X
 // and four from 16 further.
+// (volatile: two loads must not become one that needs its halves moved)
 template <int W>
 __device__ __forceinline__ Operand<bf16> split_operand(uint32_t base, int X, int off, bf16) {
-  const bf16x4 a = lds_read<bf16x4>((base ^ Rows<bf16, W>::at(0, X)) + off);
-  const bf16x4 b = lds_read<bf16x4>((base ^ Rows<bf16, W>::at(0, X + 16)) + off);
+  const bf16x4 a = lds_read<volatile bf16x4>((base ^ Rows<bf16, W>::at(0, X)) + off);
+  const bf16x4 b = lds_read<volatile bf16x4>((base ^ Rows<bf16, W>::at(0, X + 16)) + off);
   return {__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)};
 }
 template <int W>
@@ -381,6 +383,10 @@ template <int I>
 __device__ __forceinline__ float rest(float x, bf16x2 hi) {
   const uint32_t u = __builtin_bit_cast(uint32_t, hi);
   return x - __uint_as_float(I ? u & 0xffff0000u : u << 16);
+}
+__device__ __forceinline__ bf16x2 rounded(float x0, float x1) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  return __builtin_convertvector((f32x2{x0, x1}), bf16x2);
 }
 __device__ __forceinline__ bf16x2 cut(float x0, float x1) {
   return __builtin_bit_cast(
@@ -530,6 +536,7 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_state_kernel
   load_rows<T, D>(uniform_ptr(k + begin * D), kChunk, lds, wave, lane);
   v.load(vt, a.vt_ld, begin, len, wave, lane);
   uint32_t buf = lds, next = lds + R::TOTAL;
+  __builtin_amdgcn_s_waitcnt(0);
   for (int64_t c0 = begin; c0 < end; c0 += kChunk) {
     barrier_all();
     if (c0 + kChunk < end) {
@@ -589,11 +596,12 @@ __device__ __forceinline__ void state_operand(const State<D>& s, int kk, Operand
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const f32x4 t = s.t[2 * kk + (e >> 2)];
-    const bf16x2 hi = {(bf16)t[e & 3], (bf16)t[(e & 3) + 1]};
+    const float x0 = t[e & 3], x1 = t[(e & 3) + 1];
+    const bf16x2 hi = rounded(x0, x1), lo = rounded(rest<0>(x0, hi), rest<1>(x1, hi));
     out[0].v[e] = hi[0];
     out[0].v[e + 1] = hi[1];
-    out[1].v[e] = (bf16)rest<0>(t[e & 3], hi);
-    out[1].v[e + 1] = (bf16)rest<1>(t[(e & 3) + 1], hi);
+    out[1].v[e] = lo[0];
+    out[1].v[e + 1] = lo[1];
   }
 }
 template <int D>
@@ -603,21 +611,18 @@ __device__ __forceinline__ void state_operand(const State<D>& s, int kk, Operand
 
 // Four neighbouring scores of one token into LDS.
 __device__ __forceinline__ void store_scores(uint32_t at, int part_stride, f32x4 v, bf16) {
-  const bf16x2 h0 = {(bf16)v[0], (bf16)v[1]}, h1 = {(bf16)v[2], (bf16)v[3]};
-  const bf16x4 lo = {(bf16)rest<0>(v[0], h0), (bf16)rest<1>(v[1], h0), (bf16)rest<0>(v[2], h1),
-                     (bf16)rest<1>(v[3], h1)};
+  const bf16x2 h0 = rounded(v[0], v[1]), h1 = rounded(v[2], v[3]);
+  const bf16x2 l0 = rounded(rest<0>(v[0], h0), rest<1>(v[1], h0));
+  const bf16x2 l1 = rounded(rest<0>(v[2], h1), rest<1>(v[3], h1));
   lds_write(at, (bf16x4)__builtin_shufflevector(h0, h1, 0, 1, 2, 3));
-  lds_write(at + part_stride, lo);
+  lds_write(at + part_stride, (bf16x4)__builtin_shufflevector(l0, l1, 0, 1, 2, 3));
 }
 __device__ __forceinline__ void store_scores(uint32_t at, int, f32x4 v, float) {
   lds_write(at, v);
 }
 
 __device__ __forceinline__ void store_out(bf16* p, f32x4 v) {
-  bf16x4 b;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) b[i] = (bf16)v[i];
-  *reinterpret_cast<bf16x4*>(p) = b;
+  *reinterpret_cast<bf16x4*>(p) = __builtin_convertvector(v, bf16x4);
 }
 __device__ __forceinline__ void store_out(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
 
@@ -638,8 +643,11 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
   const T* q = (const T*)a.q + hs * a.tokens * D;
   const T* k = (const T*)a.k + hs * a.tokens * D;
   const T* vt = (const T*)a.vt + hs * D * a.vt_ld;
-  T* o = (T*)a.o + (seq * a.tokens * a.heads + head) * D + wave * 16;
-  // lambda^64 in two parts: a rounded factor would add up over the chunks
+  const int64_t o_ld = (int64_t)a.heads * D;
+  T* o = (T*)a.o + seq * a.tokens * o_ld + head * D + wave * 16;
+  // lambda^64, for a state in fp32 in two parts: a rounded factor would add up
+  // over the chunks
+  constexpr bool TWO_PART_DECAY = LAST || sizeof(T) == 4;
   const double whole = exp(-(double)slope * kChunk);
   const Powers pw(rate);
   const float whole_hi = uniform((float)whole);
@@ -678,12 +686,16 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
         });
       }
   }
+  float tile_decay[4];
+#pragma unroll
+  for (int tt = 0; tt < 4; ++tt) tile_decay[tt] = uniform(a.scale * exp2_fast(-rate * (float)(16 * tt)));
   // the scores' tiles of this wave: tokens 16 tq .., keys 16 st .., st from
   // st0 to st1; the tile beside an even diagonal one is written too, as zeros
   const int tq = D == 128 ? wave >> 1 : wave;
   const int st0 = D == 128 ? (tq < 2 ? wave & 1 : 2 * (wave & 1)) : 0;
   const int st1 = D == 128 ? (tq < 2 ? st0 : st0 + 1) : tq | 1;
 
+  __builtin_amdgcn_s_waitcnt(0);  // S is here: no wait for it among the chunks' loads
   int64_t c0 = begin;
   // One chunk of n tokens: 64, or (WHOLE false) a sequence's last ones.
   auto chunk = [&](auto whole_chunk, int n, bool update) {
@@ -732,8 +744,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
       __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int tt = 0; tt < 4; ++tt)
-      out[tt] *= a.scale * exp2_fast(-rate * (float)(16 * tt + col + 1));
+    for (int tt = 0; tt < 4; ++tt) out[tt] *= exp2_fast(-rate * (float)(col + 1)) * tile_decay[tt];
     barrier_lds();
 
     const uint32_t weights = afresh(scores + P::at(col, 8 * g));
@@ -748,16 +759,18 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
                                             16 * tt * P::BYTES + p * P::TOTAL, T()),
                         out[tt]);
     __builtin_amdgcn_sched_barrier(0);
+    T* at = o + c0 * o_ld + col * o_ld + 4 * g;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
-      const int64_t t = c0 + 16 * tt + col;
-      if (WHOLE || t < end) store_out(o + t * a.heads * D + 4 * g, out[tt]);
+      if (WHOLE || 16 * tt + col < n) store_out(at, out[tt]);
+      at += 16 * o_ld;
     }
     if (update) {
       if constexpr (WHOLE)
         for_state(s, [&](f32x4& t, int, int, int) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) t[i] = fmaf(t[i], whole_hi, t[i] * whole_lo);
+          for (int i = 0; i < 4; ++i)
+            t[i] = TWO_PART_DECAY ? fmaf(t[i], whole_hi, t[i] * whole_lo) : t[i] * whole_hi;
         });
       else {
         const float w = exp2_fast(-rate * (float)n);
