@@ -353,12 +353,17 @@ struct State {
 template <typename T>
 struct ValueTile {
   Operand<T> v[2];
-  __device__ __forceinline__ void load(const T* vt, int64_t vt_ld, int64_t c0, int64_t len,
-                                       int wave, int lane) {
+  // at: the lane's row, at token c0 + 8 g
+  __device__ __forceinline__ void load(const T* at, int64_t c0, int64_t len, int lane) {
+    if (c0 + kChunk <= len) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const int64_t t = c0 + 32 * ks + 8 * (lane >> 4);
-      v[ks] = load8(vt + (wave * 16 + (lane & 15)) * vt_ld + (t < len ? t : 0));
+      for (int ks = 0; ks < 2; ++ks) v[ks] = load8(at + 32 * ks);
+    } else {  // eights from len on: the chunk's first one instead, to be masked
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const int g8 = 8 * (lane >> 4);
+        v[ks] = load8(at + (c0 + 32 * ks + g8 < len ? 32 * ks : -g8));
+      }
     }
   }
   // tokens from n on become zeros
@@ -530,18 +535,18 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_state_kernel
     for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{0.f, 0.f, 0.f, 0.f}; });
   }
   const T* k = (const T*)a.k + hs * a.tokens * D;
-  const T* vt = (const T*)a.vt + hs * D * a.vt_ld;
+  const T* vt = (const T*)a.vt + (hs * D + wave * 16 + (lane & 15)) * a.vt_ld + 8 * (lane >> 4);
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_void_t*)rows;
   ValueTile<T> v, v_next;
   load_rows<T, D>(uniform_ptr(k + begin * D), kChunk, lds, wave, lane);
-  v.load(vt, a.vt_ld, begin, len, wave, lane);
+  v.load(vt + begin, begin, len, lane);
   uint32_t buf = lds, next = lds + R::TOTAL;
   __builtin_amdgcn_s_waitcnt(0);
   for (int64_t c0 = begin; c0 < end; c0 += kChunk) {
     barrier_all();
     if (c0 + kChunk < end) {
       load_rows<T, D>(uniform_ptr(k + (c0 + kChunk) * D), kChunk, next, wave, lane);
-      v_next.load(vt, a.vt_ld, c0 + kChunk, len, wave, lane);
+      v_next.load(vt + c0 + kChunk, c0 + kChunk, len, lane);
     }
     add_outer<T, D, PARTS, true>(s, afresh(buf + column_base<T, D>(lane)), v, rate, pw,
                                  (int)(end - 1 - c0), lane);
@@ -642,7 +647,8 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
 
   const T* q = (const T*)a.q + hs * a.tokens * D;
   const T* k = (const T*)a.k + hs * a.tokens * D;
-  const T* vt = (const T*)a.vt + hs * D * a.vt_ld;
+  const T* vt = (const T*)a.vt + (hs * D + wave * 16 + (threadIdx.x & 15)) * a.vt_ld +
+                8 * ((threadIdx.x & 63) >> 4);
   const int64_t o_ld = (int64_t)a.heads * D;
   T* o = (T*)a.o + seq * a.tokens * o_ld + head * D + wave * 16;
   // lambda^64, for a state in fp32 in two parts: a rounded factor would add up
@@ -659,7 +665,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     const int n = end - c0 < kChunk ? (int)(end - c0) : kChunk;
     load_rows<T, D>(uniform_ptr(q + c0 * D), n, to, wave, lane);
     load_rows<T, D>(uniform_ptr(k + c0 * D), n, to + R::TOTAL, wave, lane);
-    values.load(vt, a.vt_ld, c0, len, wave, lane);
+    values.load(vt + c0, c0, len, lane);
   };
   if (begin < end) load(begin, buf, v, threadIdx.x & 63);
 
@@ -689,12 +695,15 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
   float tile_decay[4];
 #pragma unroll
   for (int tt = 0; tt < 4; ++tt) tile_decay[tt] = uniform(a.scale * exp2_fast(-rate * (float)(16 * tt)));
-  // the scores' tiles of this wave: tokens 16 tq .., keys 16 st .., st from
-  // st0 to st1; the tile beside an even diagonal one is written too, as zeros
-  const int tq = D == 128 ? wave >> 1 : wave;
-  const int st0 = D == 128 ? (tq < 2 ? wave & 1 : 2 * (wave & 1)) : 0;
-  const int st1 = D == 128 ? (tq < 2 ? st0 : st0 + 1) : tq | 1;
-
+  // the scores' tiles of this wave, 4 tq + st a digit: tokens 16 tq .., keys 16
+  // st ..; the ten on and below the diagonal, and the two beside an even
+  // diagonal one, which are written as zeros
+  const uint32_t tiles =
+      D == 64 ? (wave == 0 ? 0xf10 : wave == 1 ? 0xe54 : wave == 2 ? 0xba98 : 0xdc)
+      : wave < 4 ? (wave == 0 ? 0x10 : wave == 1 ? 0x54 : wave == 2 ? 0x8 : 0x9)
+                 : (wave == 4 ? 0xba : wave == 5 ? 0xdc : wave == 6 ? 0xe : 0xf);
+  const int n_tiles = D == 64 ? (wave == 2 ? 4 : wave == 3 ? 2 : 3)
+                              : (wave < 2 || wave == 4 || wave == 5 ? 2 : 1);
   __builtin_amdgcn_s_waitcnt(0);  // S is here: no wait for it among the chunks' loads
   int64_t c0 = begin;
   // One chunk of n tokens: 64, or (WHOLE false) a sequence's last ones.
@@ -707,7 +716,8 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     if (!WHOLE) v.mask(n, lane);
 
     const uint32_t along = afresh(buf + R::at(col, 4 * g));
-    for (int st = st0; st <= st1; ++st) {
+    for (int i = 0; i < n_tiles; ++i) {
+      const int tq = tiles >> (4 * i + 2) & 3, st = tiles >> (4 * i) & 3;
       f32x4 p = {0.f, 0.f, 0.f, 0.f};
       if (st <= tq) {
         const uint32_t k_at = (along ^ R::tile_bits(st)) + R::TOTAL + 16 * st * R::BYTES;
