@@ -171,49 +171,73 @@ def linear(a, wt, kind: int, bias, gate=None, out=None, v_out=None, q=None, k=No
 
 
 # ------------------------------------------------ linear-attention block
+#
+# A call for a few tokens is bound by the host, so what these functions do per
+# tensor is kept short: one test that holds, its parts only where it does not.
 
 
 def _dtype_code(t, name: str) -> int:
     torch = _torch()
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return ACID_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return ACID_F32
     raise ValueError(f"{name}: expected bfloat16 or float32, got {t.dtype}")
 
 
-def _expect(device, name: str, t, shape, dtype) -> None:
-    """t (if given) is a contiguous device tensor of this shape and type."""
+def _device(t, name: str):
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a tensor on a GPU, got one on {t.device}")
+    return t.device
+
+
+def _at(dev, name: str, t, shape: tuple, dtype) -> Optional[int]:
+    """Address of t (or None): a contiguous tensor on dev of this shape and type."""
     if t is None:
-        return
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name}: expected a tensor on {device}, got {t.device}")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)}, "
-                         f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+        return None
+    if t.shape == shape and t.dtype is dtype and t.device == dev and t.is_contiguous():
+        return t.data_ptr()
+    if t.device != dev:
+        raise ValueError(f"{name}: expected a tensor on {dev}, got {t.device}")
+    raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape}, "
+                     f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
-def _rows(device, name: str, t, rows: int, cols: int):
-    """(address, row stride) of a [rows, cols] device tensor of unit column
-    stride; a row stride that no row uses is given as whole rows."""
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name}: expected a tensor on {device}, got {t.device}")
-    if tuple(t.shape) != (rows, cols):
-        raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: expected unit column stride, got {t.stride()}")
-    if rows > 1 and t.stride(0) < cols:
-        raise ValueError(f"{name}: rows overlap (strides {t.stride()})")
-    return C.c_void_p(t.data_ptr()), (t.stride(0) if rows > 1 else (cols + 7) // 8 * 8)
+def _rows_at(dev, name: str, t, shape: tuple, dtype):
+    """(address, row stride) of a matrix on dev of this shape and type, of unit
+    column stride; of one row the stride counts as whole 16 bytes."""
+    ld, unit = t.stride() if t.dim() == 2 else (0, 0)
+    rows, cols = shape
+    if t.shape == shape and t.dtype is dtype and t.device == dev:
+        if rows > 1 and unit == 1 and ld >= cols:
+            return t.data_ptr(), ld
+        if rows <= 1 and (unit == 1 or cols == 1):
+            return t.data_ptr(), (cols + 7) // 8 * 8
+        if cols == 1 and ld >= 1:
+            return t.data_ptr(), ld
+        raise ValueError(f"{name}: expected unit column stride and rows apart, got strides {t.stride()}")
+    if t.device != dev:
+        raise ValueError(f"{name}: expected a tensor on {dev}, got {t.device}")
+    raise ValueError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)}")
 
 
-def _stream_of(device, stream):
-    """The stream a call on `device` runs on: the one given, which has to be
-    that device's, or the device's current one."""
-    s = stream if stream is not None else _torch().cuda.current_stream(device)
-    if s.device != device:
-        raise ValueError(f"stream of {s.device} for tensors on {device}")
-    return s
+def _on(dev, stream, fn, *args) -> None:
+    """fn(*args, stream) on `dev`: the stream given, which has to be that
+    device's, or its current one."""
+    torch = _torch()
+    if stream is not None:
+        if stream.device != dev:
+            raise ValueError(f"stream of {stream.device} for tensors on {dev}")
+        raw = stream.cuda_stream
+    else:
+        raw = torch._C._cuda_getCurrentRawStream(dev.index)
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):  # what the null stream means
+            status = fn(*args, raw)
+    else:
+        status = fn(*args, raw)
+    if status:
+        check(status)
 
 
 def linear_attention_workspace(n_seq: int, n_heads: int, seq_len: int, head_dim: int) -> int:
@@ -235,34 +259,29 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
     torch = _torch()
     if q.dim() not in (3, 4):
         raise ValueError("q: expected [heads, L, d] or [n_seq, heads, L, d]")
-    code, dev, lead = _dtype_code(q, "q"), q.device, tuple(q.shape[:-3])
+    code, dev, lead, dt = _dtype_code(q, "q"), _device(q, "q"), tuple(q.shape[:-3]), q.dtype
     n_heads, L, d = q.shape[-3:]
     n_seq = lead[0] if lead else 1
     if vt.dim() != q.dim():
         raise ValueError("vt: expected as many axes as q")
-    _expect(dev, "q", q, q.shape, q.dtype)
-    _expect(dev, "k", k, q.shape, q.dtype)
-    _expect(dev, "vt", vt, lead + (n_heads, d, vt.shape[-1]), q.dtype)
-    _expect(dev, "o", o, lead + (L, n_heads * d), q.dtype)
-    _expect(dev, "slopes", slopes, (n_heads,), torch.float32)
-    for name, t in (("state_in", state_in), ("state_out", state_out)):
-        _expect(dev, name, t, lead + (n_heads, d, d), torch.float32)
-    _expect(dev, "lengths", lengths, (n_seq,), torch.int32)
-    s = _stream_of(dev, stream)
+    states, vt_ld = lead + (n_heads, d, d), vt.shape[-1]
+    args = (_at(dev, "q", q, lead + (n_heads, L, d), dt), _at(dev, "k", k, lead + (n_heads, L, d), dt),
+            _at(dev, "vt", vt, lead + (n_heads, d, vt_ld), dt), vt_ld,
+            _at(dev, "slopes", slopes, (n_heads,), torch.float32),
+            _at(dev, "lengths", lengths, (n_seq,), torch.int32),
+            _at(dev, "state_in", state_in, states, torch.float32),
+            _at(dev, "state_out", state_out, states, torch.float32),
+            d ** -0.5 if scale is None else scale,
+            _at(dev, "o", o, lead + (L, n_heads * d), dt))
     if workspace is None:
-        need = linear_attention_workspace(n_seq, n_heads, L, d)
-        if need:
-            with torch.cuda.stream(s):  # its memory goes back to this stream's pool
-                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    elif workspace.dtype != torch.uint8:
-        raise ValueError("workspace: expected a uint8 tensor")
+        size = lib().acid_linear_attention_workspace_bytes(n_seq, n_heads, L, d)
+        if size:
+            with torch.cuda.stream(stream):  # its memory goes back to that stream's pool
+                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
     else:
-        _expect(dev, "workspace", workspace, workspace.shape, torch.uint8)
-    check(lib().acid_linear_attention(
-        code, n_seq, n_heads, L, d, _ptr(q), _ptr(k), _ptr(vt), vt.shape[-1], _ptr(slopes),
-        _ptr(lengths), _ptr(state_in), _ptr(state_out),
-        float(d ** -0.5 if scale is None else scale), _ptr(o), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), C.c_void_p(s.cuda_stream)))
+        size = workspace.numel()
+    _on(dev, stream, lib().acid_linear_attention, code, n_seq, n_heads, L, d, *args,
+        None if workspace is None else _at(dev, "workspace", workspace, (size,), torch.uint8), size)
 
 
 def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
@@ -276,24 +295,17 @@ def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
     torch = _torch()
     if state.dim() != 4:
         raise ValueError("state: expected [n_slots, heads, d, d]")
-    code, dev = _dtype_code(q, "q"), state.device
-    n_slots, n_heads, d, _ = state.shape
-    rows = q.shape[0]
-    out = state if state_out is None else state_out
-    _expect(dev, "state", state, (n_slots, n_heads, d, d), torch.float32)
-    _expect(dev, "state_out", out, (n_slots, n_heads, d, d), torch.float32)
-    _expect(dev, "slopes", slopes, (n_heads,), torch.float32)
-    _expect(dev, "slots", slots, (rows,), torch.int32)
-    args = []
-    for name, t in (("q", q), ("k", k), ("v", v), ("o", o)):
-        if t.dtype != q.dtype:
-            raise ValueError(f"{name}: expected {q.dtype}, got {t.dtype}")
-        args.append(_rows(dev, name, t, rows, n_heads * d))
-    s = _stream_of(dev, stream)
-    check(lib().acid_linear_attention_step(
-        code, rows, n_heads, d, *args[0], *args[1], *args[2], _ptr(slopes), _ptr(slots), n_slots,
-        _ptr(state), _ptr(out), float(d ** -0.5 if scale is None else scale), *args[3],
-        C.c_void_p(s.cuda_stream)))
+    code, dev, dt = _dtype_code(q, "q"), _device(state, "state"), q.dtype
+    n_slots, n_heads, d = state.shape[:3]
+    rows, states = q.shape[0], (n_slots, n_heads, d, d)
+    shape = (rows, n_heads * d)
+    at = _at(dev, "state", state, states, torch.float32)
+    _on(dev, stream, lib().acid_linear_attention_step, code, rows, n_heads, d,
+        *_rows_at(dev, "q", q, shape, dt), *_rows_at(dev, "k", k, shape, dt),
+        *_rows_at(dev, "v", v, shape, dt), _at(dev, "slopes", slopes, (n_heads,), torch.float32),
+        _at(dev, "slots", slots, (rows,), torch.int32), n_slots, at,
+        at if state_out is None else _at(dev, "state_out", state_out, states, torch.float32),
+        d ** -0.5 if scale is None else scale, *_rows_at(dev, "o", o, shape, dt))
 
 
 _NORMS = {"none": ACID_NORM_NONE, "layer": ACID_NORM_LAYER, "rms": ACID_NORM_RMS}
@@ -309,43 +321,34 @@ def residual_norm(h, y=None, h_out=None, out=None, res_scale: float = 1.0, post:
     [hidden]; gate, shift, scale fp32 [hidden], or [n_mod, hidden] with row r
     using row r // rows_per_mod.  Matrices may be row-strided."""
     torch = _torch()
-    if h.dim() != 2 or h.dtype != torch.float32:
-        raise ValueError("h: expected an fp32 [rows, hidden] tensor")
-    for kind in (post, pre):
-        if kind not in _NORMS:
-            raise ValueError(f"unknown norm {kind!r}")
+    f32 = torch.float32
+    if post not in _NORMS or pre not in _NORMS:
+        raise ValueError(f"unknown norm {post if post not in _NORMS else pre!r}")
     if rows_per_mod < 0:
         raise ValueError("rows_per_mod < 0")
-    dev, (rows, hidden) = h.device, h.shape
+    if h.dim() != 2:
+        raise ValueError("h: expected [rows, hidden]")
     if y is None and h_out is not None:
         raise ValueError("h_out without y")
-    if h_out is None:
-        h_out = h
-    elif h_out.dtype != torch.float32:
-        raise ValueError("h_out: expected fp32")
-    a = _L.ResidualNormArgsC()
-    a.h, a.h_ld = _rows(dev, "h", h, rows, hidden)
-    if y is not None:
-        a.y_dtype = _dtype_code(y, "y")
-        a.y, a.y_ld = _rows(dev, "y", y, rows, hidden)
-        a.h_out, a.h_out_ld = _rows(dev, "h_out", h_out, rows, hidden)
-    if out is not None:
-        a.out_dtype = _dtype_code(out, "out")
-        a.out, a.out_ld = _rows(dev, "out", out, rows, hidden)
+    dev, shape = _device(h, "h"), tuple(h.shape)
+    rows, hidden = shape
     n_mod = -(-rows // rows_per_mod) if rows_per_mod else 1
-    for name, t in (("post_weight", post_weight), ("pre_weight", pre_weight)):
-        _expect(dev, name, t, (hidden,), torch.float32)
-    for name, t in (("gate", gate), ("shift", shift), ("scale", scale)):
-        if t is not None and t.dim() == 1 and n_mod == 1:
-            _expect(dev, name, t, (hidden,), torch.float32)
-        else:
-            _expect(dev, name, t, (n_mod, hidden), torch.float32)
-    a.post_weight, a.pre_weight = _ptr(post_weight), _ptr(pre_weight)
-    a.gate, a.shift, a.scale = _ptr(gate), _ptr(shift), _ptr(scale)
-    a.post, a.pre = _NORMS[post], _NORMS[pre]
-    a.rows_per_mod, a.res_scale, a.eps = int(rows_per_mod), float(res_scale), float(eps)
-    s = _stream_of(dev, stream)
-    check(lib().acid_residual_norm(C.byref(a), rows, hidden, C.c_void_p(s.cuda_stream)))
+    nothing = (None, 0)
+
+    def vector(name, t):
+        one = t is not None and n_mod == 1 and t.dim() == 1
+        return _at(dev, name, t, (hidden,) if one else (n_mod, hidden), f32)
+
+    h_at = _rows_at(dev, "h", h, shape, f32)
+    a = _L.ResidualNormArgsC(
+        *h_at, *(nothing if y is None else _rows_at(dev, "y", y, shape, y.dtype)),
+        *(h_at if h_out is None else _rows_at(dev, "h_out", h_out, shape, f32)),
+        *(nothing if out is None else _rows_at(dev, "out", out, shape, out.dtype)),
+        0 if y is None else _dtype_code(y, "y"), 0 if out is None else _dtype_code(out, "out"),
+        _NORMS[post], _NORMS[pre], _at(dev, "post_weight", post_weight, (hidden,), f32),
+        _at(dev, "pre_weight", pre_weight, (hidden,), f32), vector("gate", gate),
+        vector("shift", shift), vector("scale", scale), rows_per_mod, res_scale, eps)
+    _on(dev, stream, lib().acid_residual_norm, a, rows, hidden)
 
 
 def w4_shapes(n: int, k: int, group: int = 128):
@@ -357,48 +360,40 @@ def w4_shapes(n: int, k: int, group: int = 128):
     return (tiles, k // 128, 64, 16), (tiles, k // group, 16)
 
 
-def _w4_group(codes, scales, k: int):
-    if codes.dim() != 4 or scales.dim() != 3 or scales.shape[1] < 1 or k % scales.shape[1]:
+def _w4_at(x, codes, scales, n: int, k: int):
+    """(x's device, group, codes' address, scales' address)."""
+    groups = scales.shape[1] if scales.dim() == 3 else 0
+    if groups < 1 or k % groups or codes.dim() != 4:
         raise ValueError("codes, scales: see w4_shapes")
-    return k // scales.shape[1]
+    torch, group = _torch(), k // groups
+    cs, ss = w4_shapes(n, k, group)
+    dev = _device(x, "x")
+    return dev, group, _at(dev, "codes", codes, cs, torch.uint8), _at(dev, "scales", scales, ss, torch.float32)
 
 
 def quantize_w4(w, codes, scales, stream=None) -> None:
     """codes, scales (w4_shapes) of the fp32 weight w [k inputs, n outputs]."""
-    torch = _torch()
     if w.dim() != 2:
         raise ValueError("w: expected [k, n]")
-    (k, n), dev = w.shape, w.device
-    group = _w4_group(codes, scales, k)
-    cs, ss = w4_shapes(n, k, group)
-    _expect(dev, "w", w, (k, n), torch.float32)
-    _expect(dev, "codes", codes, cs, torch.uint8)
-    _expect(dev, "scales", scales, ss, torch.float32)
-    s = _stream_of(dev, stream)
-    check(lib().acid_quantize_w4(_ptr(w), n, k, group, _ptr(codes), _ptr(scales),
-                                 C.c_void_p(s.cuda_stream)))
+    k, n = w.shape
+    dev, group, c, s = _w4_at(w, codes, scales, n, k)
+    _on(dev, stream, lib().acid_quantize_w4, _at(dev, "w", w, (k, n), _torch().float32), n, k, group,
+        c, s)
 
 
 def linear_w4(x, codes, scales, out, bias=None, gelu: bool = False, stream=None) -> None:
     """out = act(x w^T + bias) for few rows x [m, k] (bf16 or fp32) and 4-bit
     weights (quantize_w4); out [m, n] bf16 or fp32; bias fp32 [n].  x and out
     may be row-strided."""
-    torch = _torch()
     if x.dim() != 2 or out.dim() != 2:
         raise ValueError("x and out: expected two axes")
-    (m, k), n, dev = x.shape, out.shape[1], x.device
-    group = _w4_group(codes, scales, k)
-    cs, ss = w4_shapes(n, k, group)
-    _expect(dev, "codes", codes, cs, torch.uint8)
-    _expect(dev, "scales", scales, ss, torch.float32)
-    _expect(dev, "bias", bias, (n,), torch.float32)
-    xp, x_ld = _rows(dev, "x", x, m, k)
-    op, out_ld = _rows(dev, "out", out, m, n)
-    s = _stream_of(dev, stream)
-    check(lib().acid_linear_w4(_dtype_code(x, "x"), m, n, k, group, xp, x_ld, _ptr(codes),
-                               _ptr(scales), _ptr(bias),
-                               ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS,
-                               _dtype_code(out, "out"), op, out_ld, C.c_void_p(s.cuda_stream)))
+    (m, k), n = x.shape, out.shape[1]
+    dev, group, c, s = _w4_at(x, codes, scales, n, k)
+    _on(dev, stream, lib().acid_linear_w4, _dtype_code(x, "x"), m, n, k, group,
+        *_rows_at(dev, "x", x, (m, k), x.dtype), c, s,
+        _at(dev, "bias", bias, (n,), _torch().float32),
+        ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS, _dtype_code(out, "out"),
+        *_rows_at(dev, "out", out, (m, n), out.dtype))
 
 
 # ------------------------------------------------------------------ model
