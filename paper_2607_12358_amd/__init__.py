@@ -176,11 +176,11 @@ def linear(a, wt, kind: int, bias, gate=None, out=None, v_out=None, q=None, k=No
 # tensor is kept short: one test that holds, its parts only where it does not.
 
 
-def _dtype_code(t, name: str) -> int:
-    torch = _torch()
-    if t.dtype is torch.bfloat16:
+def _dtype_code(torch, t, name: str) -> int:
+    dtype = t.dtype
+    if dtype is torch.bfloat16:
         return ACID_BF16
-    if t.dtype is torch.float32:
+    if dtype is torch.float32:
         return ACID_F32
     raise ValueError(f"{name}: expected bfloat16 or float32, got {t.dtype}")
 
@@ -206,25 +206,23 @@ def _at(dev, name: str, t, shape: tuple, dtype) -> Optional[int]:
 def _rows_at(dev, name: str, t, shape: tuple, dtype):
     """(address, row stride) of a matrix on dev of this shape and type, of unit
     column stride; of one row the stride counts as whole 16 bytes."""
-    ld, unit = t.stride() if t.dim() == 2 else (0, 0)
-    rows, cols = shape
     if t.shape == shape and t.dtype is dtype and t.device == dev:
-        if rows > 1 and unit == 1 and ld >= cols:
-            return t.data_ptr(), ld
-        if rows <= 1 and (unit == 1 or cols == 1):
-            return t.data_ptr(), (cols + 7) // 8 * 8
-        if cols == 1 and ld >= 1:
-            return t.data_ptr(), ld
+        rows, cols = shape
+        ld, unit = t.stride()
+        if unit == 1 or cols == 1:
+            if rows <= 1:
+                return t.data_ptr(), (cols + 7) // 8 * 8
+            if ld >= cols:
+                return t.data_ptr(), ld
         raise ValueError(f"{name}: expected unit column stride and rows apart, got strides {t.stride()}")
     if t.device != dev:
         raise ValueError(f"{name}: expected a tensor on {dev}, got {t.device}")
     raise ValueError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)}")
 
 
-def _on(dev, stream, fn, *args) -> None:
+def _on(torch, dev, stream, fn, *args) -> None:
     """fn(*args, stream) on `dev`: the stream given, which has to be that
     device's, or its current one."""
-    torch = _torch()
     if stream is not None:
         if stream.device != dev:
             raise ValueError(f"stream of {stream.device} for tensors on {dev}")
@@ -259,7 +257,7 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
     torch = _torch()
     if q.dim() not in (3, 4):
         raise ValueError("q: expected [heads, L, d] or [n_seq, heads, L, d]")
-    code, dev, lead, dt = _dtype_code(q, "q"), _device(q, "q"), tuple(q.shape[:-3]), q.dtype
+    code, dev, lead, dt = _dtype_code(torch, q, "q"), _device(q, "q"), tuple(q.shape[:-3]), q.dtype
     n_heads, L, d = q.shape[-3:]
     n_seq = lead[0] if lead else 1
     if vt.dim() != q.dim():
@@ -280,7 +278,7 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
                 workspace = torch.empty(size, dtype=torch.uint8, device=dev)
     else:
         size = workspace.numel()
-    _on(dev, stream, lib().acid_linear_attention, code, n_seq, n_heads, L, d, *args,
+    _on(torch, dev, stream, lib().acid_linear_attention, code, n_seq, n_heads, L, d, *args,
         None if workspace is None else _at(dev, "workspace", workspace, (size,), torch.uint8), size)
 
 
@@ -295,12 +293,12 @@ def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
     torch = _torch()
     if state.dim() != 4:
         raise ValueError("state: expected [n_slots, heads, d, d]")
-    code, dev, dt = _dtype_code(q, "q"), _device(state, "state"), q.dtype
+    code, dev, dt = _dtype_code(torch, q, "q"), _device(state, "state"), q.dtype
     n_slots, n_heads, d = state.shape[:3]
     rows, states = q.shape[0], (n_slots, n_heads, d, d)
     shape = (rows, n_heads * d)
     at = _at(dev, "state", state, states, torch.float32)
-    _on(dev, stream, lib().acid_linear_attention_step, code, rows, n_heads, d,
+    _on(torch, dev, stream, lib().acid_linear_attention_step, code, rows, n_heads, d,
         *_rows_at(dev, "q", q, shape, dt), *_rows_at(dev, "k", k, shape, dt),
         *_rows_at(dev, "v", v, shape, dt), _at(dev, "slopes", slopes, (n_heads,), torch.float32),
         _at(dev, "slots", slots, (rows,), torch.int32), n_slots, at,
@@ -344,11 +342,11 @@ def residual_norm(h, y=None, h_out=None, out=None, res_scale: float = 1.0, post:
         *h_at, *(nothing if y is None else _rows_at(dev, "y", y, shape, y.dtype)),
         *(h_at if h_out is None else _rows_at(dev, "h_out", h_out, shape, f32)),
         *(nothing if out is None else _rows_at(dev, "out", out, shape, out.dtype)),
-        0 if y is None else _dtype_code(y, "y"), 0 if out is None else _dtype_code(out, "out"),
+        0 if y is None else _dtype_code(torch, y, "y"), 0 if out is None else _dtype_code(torch, out, "out"),
         _NORMS[post], _NORMS[pre], _at(dev, "post_weight", post_weight, (hidden,), f32),
         _at(dev, "pre_weight", pre_weight, (hidden,), f32), vector("gate", gate),
         vector("shift", shift), vector("scale", scale), rows_per_mod, res_scale, eps)
-    _on(dev, stream, lib().acid_residual_norm, a, rows, hidden)
+    _on(torch, dev, stream, lib().acid_residual_norm, a, rows, hidden)
 
 
 def w4_shapes(n: int, k: int, group: int = 128):
@@ -360,12 +358,12 @@ def w4_shapes(n: int, k: int, group: int = 128):
     return (tiles, k // 128, 64, 16), (tiles, k // group, 16)
 
 
-def _w4_at(x, codes, scales, n: int, k: int):
+def _w4_at(torch, x, codes, scales, n: int, k: int):
     """(x's device, group, codes' address, scales' address)."""
     groups = scales.shape[1] if scales.dim() == 3 else 0
     if groups < 1 or k % groups or codes.dim() != 4:
         raise ValueError("codes, scales: see w4_shapes")
-    torch, group = _torch(), k // groups
+    group = k // groups
     cs, ss = w4_shapes(n, k, group)
     dev = _device(x, "x")
     return dev, group, _at(dev, "codes", codes, cs, torch.uint8), _at(dev, "scales", scales, ss, torch.float32)
@@ -373,11 +371,12 @@ def _w4_at(x, codes, scales, n: int, k: int):
 
 def quantize_w4(w, codes, scales, stream=None) -> None:
     """codes, scales (w4_shapes) of the fp32 weight w [k inputs, n outputs]."""
+    torch = _torch()
     if w.dim() != 2:
         raise ValueError("w: expected [k, n]")
     k, n = w.shape
-    dev, group, c, s = _w4_at(w, codes, scales, n, k)
-    _on(dev, stream, lib().acid_quantize_w4, _at(dev, "w", w, (k, n), _torch().float32), n, k, group,
+    dev, group, c, s = _w4_at(torch, w, codes, scales, n, k)
+    _on(torch, dev, stream, lib().acid_quantize_w4, _at(dev, "w", w, (k, n), torch.float32), n, k, group,
         c, s)
 
 
@@ -385,14 +384,15 @@ def linear_w4(x, codes, scales, out, bias=None, gelu: bool = False, stream=None)
     """out = act(x w^T + bias) for few rows x [m, k] (bf16 or fp32) and 4-bit
     weights (quantize_w4); out [m, n] bf16 or fp32; bias fp32 [n].  x and out
     may be row-strided."""
+    torch = _torch()
     if x.dim() != 2 or out.dim() != 2:
         raise ValueError("x and out: expected two axes")
     (m, k), n = x.shape, out.shape[1]
-    dev, group, c, s = _w4_at(x, codes, scales, n, k)
-    _on(dev, stream, lib().acid_linear_w4, _dtype_code(x, "x"), m, n, k, group,
+    dev, group, c, s = _w4_at(torch, x, codes, scales, n, k)
+    _on(torch, dev, stream, lib().acid_linear_w4, _dtype_code(torch, x, "x"), m, n, k, group,
         *_rows_at(dev, "x", x, (m, k), x.dtype), c, s,
-        _at(dev, "bias", bias, (n,), _torch().float32),
-        ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS, _dtype_code(out, "out"),
+        _at(dev, "bias", bias, (n,), torch.float32),
+        ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS, _dtype_code(torch, out, "out"),
         *_rows_at(dev, "out", out, (m, n), out.dtype))
 
 
