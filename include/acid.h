@@ -531,7 +531,7 @@ typedef struct {
  *   out   = (N_pre(h_out) pre_weight) (1 + scale) + shift
  * (without y, out is made from h itself).  Row r uses row r / rows_per_mod of
  * gate, shift and scale.  h, h_out and statistics fp32.  hidden % 4 == 0,
- * <= 16384; rows <= 2^23; row strides in elements, multiples of 4; matrices
+ * <= 8192; rows <= 2^23; row strides in elements, multiples of 4; matrices
  * aligned to four of their elements, vectors to 16 bytes; outputs apart from
  * everything but h_out from h (columns of one matrix may interleave). */
 acid_status acid_residual_norm(const acid_residual_norm_args* args, int64_t rows,

@@ -32,10 +32,23 @@ struct Absent {};  // no y, or no out
 __device__ __forceinline__ float4 load4(const float* p) {
   return *reinterpret_cast<const float4*>(p);
 }
-__device__ __forceinline__ float4 load4(const bf16* p) {
-  const bf16x4 v = *reinterpret_cast<const bf16x4*>(p);
-  return make_float4((float)v[0], (float)v[1], (float)v[2], (float)v[3]);
-}
+// Four neighbouring values as they were loaded.
+template <typename T>
+struct Four {};
+template <>
+struct Four<float> {
+  float4 v;
+  __device__ __forceinline__ void load(const float* p) { v = load4(p); }
+  __device__ __forceinline__ float4 value() const { return v; }
+};
+template <>
+struct Four<bf16> {
+  bf16x4 v;
+  __device__ __forceinline__ void load(const bf16* p) { v = *reinterpret_cast<const bf16x4*>(p); }
+  __device__ __forceinline__ float4 value() const {
+    return make_float4((float)v[0], (float)v[1], (float)v[2], (float)v[3]);
+  }
+};
 __device__ __forceinline__ void store4(float* p, float4 v) { *reinterpret_cast<float4*>(p) = v; }
 __device__ __forceinline__ void store4(bf16* p, float4 v) {
   bf16x4 b;
@@ -50,10 +63,25 @@ __device__ __forceinline__ float4 mul4(float4 a, float4 b) {
   return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w);
 }
 
-// Sum of v over the WAVES waves of a row; `part` is one LDS array per sum.
+// Sum over a wave, in every lane: neighbours, fours, eights and rows of 16
+// within the vector unit (each __shfl would take a trip through LDS).
+__device__ __forceinline__ float lane_sum(float v) {
+#define ADD_DPP(ctrl, rows)                                                                    \
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), ctrl, rows, 0xf, false))
+  ADD_DPP(0x111, 0xf);  // from the lane 1 before, in its row of 16
+  ADD_DPP(0x112, 0xf);  // 2
+  ADD_DPP(0x114, 0xf);  // 4
+  ADD_DPP(0x118, 0xf);  // 8: the last lane of each row has its row's sum
+  ADD_DPP(0x142, 0xa);  // rows 1 and 3 add the row before theirs
+  ADD_DPP(0x143, 0xc);  // rows 2 and 3 add the first two
+#undef ADD_DPP
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+
+// Sum over the WAVES waves of a row; `part` is one LDS array per sum.
 template <int WAVES>
 __device__ __forceinline__ float row_sum(float v, float* part) {
-  v = wave_sum(v);
+  v = lane_sum(v);
   if constexpr (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -64,95 +92,131 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
-// v = N(v) (.) weight over a row of H values in CHUNKS float4 per thread.
-// Statistics in fp32, in two passes over the registers (mean, then centred
-// squares).  Threads past the row's end hold zeros and are left out.
+// v = N(v) over a row of H values in CHUNKS float4 per thread.  Statistics in
+// fp32, in two passes over the registers (mean, then centred squares).
+// Threads past the row's end hold copies and are left out of the sums.
 template <int WAVES, int CHUNKS>
 __device__ __forceinline__ void normalise(float4 (&v)[CHUNKS], int kind, int tid, int n4, float H,
-                                          float eps, const float* __restrict__ weight,
-                                          float (*part)[WAVES]) {
-  if (kind != ACID_NORM_NONE) {
-    float mean = 0.f;
-    if (kind == ACID_NORM_LAYER) {
-      float s = 0.f;
+                                          float eps, float (*part)[WAVES]) {
+  if (kind == ACID_NORM_NONE) return;
+  float mean = 0.f;
+  if (kind == ACID_NORM_LAYER) {
+    float s = 0.f;
 #pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) s += sum4(v[c]);
-      mean = row_sum<WAVES>(s, part[0]) / H;
-    }
-    float q = 0.f;
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      v[c] = make_float4(v[c].x - mean, v[c].y - mean, v[c].z - mean, v[c].w - mean);
-      const float t = sum4(mul4(v[c], v[c]));
-      q += tid + 64 * WAVES * c < n4 ? t : 0.f;
-    }
-    const float r = 1.0f / sqrtf(row_sum<WAVES>(q, part[1]) / H + eps);
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) v[c] = mul4(v[c], make_float4(r, r, r, r));
+    for (int c = 0; c < CHUNKS; ++c) s += tid + 64 * WAVES * c < n4 ? sum4(v[c]) : 0.f;
+    mean = row_sum<WAVES>(s, part[0]) / H;
   }
-  if (weight) {
+  float q = 0.f;
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      const int i = tid + 64 * WAVES * c;
-      if (i < n4) v[c] = mul4(v[c], load4(weight + 4 * i));
-    }
+  for (int c = 0; c < CHUNKS; ++c) {
+    v[c] = make_float4(v[c].x - mean, v[c].y - mean, v[c].z - mean, v[c].w - mean);
+    q += tid + 64 * WAVES * c < n4 ? sum4(mul4(v[c], v[c])) : 0.f;
   }
+  const float r = 1.0f / sqrtf(row_sum<WAVES>(q, part[1]) / H + eps);
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) v[c] = mul4(v[c], make_float4(r, r, r, r));
 }
 
+// A workgroup of WAVES waves takes a run of `per` rows, one after the other.
+// What the rows share (gate and post_weight as one factor, pre_weight and
+// 1 + scale as one, shift) is read once a run, or where the modulation row
+// changes, and the next row is loaded while a row is worked on: with all of it
+// read for each row (the same bytes again from L2, three dependent waits a
+// row) 32760 rows of 1536 took 145 us.  Loads past a row's end are of its last
+// chunk, so that none of them waits under a branch; what they give is neither
+// summed nor stored.
 template <int WAVES, int CHUNKS, typename Y, typename Out>
-__global__ __launch_bounds__(256) void residual_norm_kernel(NormArgs a) {
-  constexpr int ROWS = 4 / WAVES;  // rows of a workgroup
-  __shared__ float part[4][WAVES];
-  const int64_t row = (int64_t)blockIdx.x * ROWS + (WAVES == 1 ? threadIdx.x >> 6 : 0);
-  const int tid = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
-  if (row >= a.rows) return;  // whole waves; with WAVES > 1 never
+__global__ __launch_bounds__(64 * WAVES) void residual_norm_kernel(NormArgs a, int per) {
+  constexpr bool HAS_Y = !std::is_same_v<Y, Absent>, HAS_OUT = !std::is_same_v<Out, Absent>;
+  __shared__ float part[2][4][WAVES];
+  const int tid = threadIdx.x;
+  int64_t row = (int64_t)blockIdx.x * per;
+  const int64_t end = row + per < a.rows ? row + per : a.rows;
   const int n4 = a.hidden >> 2;
-  const int64_t mod = a.rows_per_mod ? row / a.rows_per_mod : 0;
   const float H = (float)a.hidden;
-
-  float4 h[CHUNKS];
+  int at[CHUNKS];
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int i = tid + 64 * WAVES * c;
-    h[c] = i < n4 ? load4(a.h + row * a.h_ld + 4 * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+    at[c] = 4 * (i < n4 ? i : n4 - 1);
   }
-  if constexpr (!std::is_same_v<Y, Absent>) {
-    float4 y[CHUNKS];
+
+  float4 h[CHUNKS], h_next[CHUNKS], y[CHUNKS];
+  Four<Y> y_next[CHUNKS];
+  float4 behind[CHUNKS], before[CHUNKS], shift[CHUNKS];
+  auto load_row = [&](int64_t r) {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      const int i = tid + 64 * WAVES * c;
-      y[c] = i < n4 ? load4((const Y*)a.y + row * a.y_ld + 4 * i)
-                    : make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c = 0; c < CHUNKS; ++c) h_next[c] = load4(a.h + r * a.h_ld + at[c]);
+    if constexpr (HAS_Y) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) y_next[c].load((const Y*)a.y + r * a.y_ld + at[c]);
     }
-    normalise<WAVES, CHUNKS>(y, a.post, tid, n4, H, a.eps, a.post_weight, part);
+  };
+  auto load_mod = [&](int64_t mod) {
+    float4 post[CHUNKS], pre[CHUNKS];
+    auto load = [&](const float* p, int64_t r, float other, float4(&to)[CHUNKS]) {
+      if (p) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) to[c] = load4(p + r * a.hidden + at[c]);
+      } else {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) to[c] = make_float4(other, other, other, other);
+      }
+    };
+    if constexpr (HAS_Y) {
+      load(a.gate, mod, 1.f, behind);
+      load(a.post_weight, 0, 1.f, post);
+    }
+    if constexpr (HAS_OUT) {
+      load(a.scale, mod, 0.f, before);
+      load(a.pre_weight, 0, 1.f, pre);
+      load(a.shift, mod, 0.f, shift);
+    }
+    if constexpr (HAS_Y) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) behind[c] = mul4(behind[c], post[c]);
+    }
+    if constexpr (HAS_OUT) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c)
+        before[c] = mul4(pre[c], make_float4(1.f + before[c].x, 1.f + before[c].y,
+                                             1.f + before[c].z, 1.f + before[c].w));
+    }
+  };
+  load_row(row);
+  int64_t mod = a.rows_per_mod ? row / a.rows_per_mod - 1 : -1, mod_end = row;
+  for (int parity = 0; row < end; ++row, parity ^= 1) {
+    if (row == mod_end) {  // the first row too
+      load_mod(++mod);
+      mod_end = a.rows_per_mod ? (mod + 1) * a.rows_per_mod : a.rows;
+    }
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-      const int i = tid + 64 * WAVES * c;
-      if (i < n4) {
-        if (a.gate) y[c] = mul4(y[c], load4(a.gate + mod * a.hidden + 4 * i));
-        h[c] = make_float4(fmaf(a.res_scale, h[c].x, y[c].x), fmaf(a.res_scale, h[c].y, y[c].y),
-                           fmaf(a.res_scale, h[c].z, y[c].z), fmaf(a.res_scale, h[c].w, y[c].w));
-        store4(a.h_out + row * a.h_out_ld + 4 * i, h[c]);
+      h[c] = h_next[c];
+      if constexpr (HAS_Y) y[c] = y_next[c].value();
+    }
+    if (row + 1 < end) load_row(row + 1);
+    if constexpr (HAS_Y) {
+      normalise<WAVES, CHUNKS>(y, a.post, tid, n4, H, a.eps, part[parity]);
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        h[c] = make_float4(fmaf(a.res_scale, h[c].x, y[c].x * behind[c].x),
+                           fmaf(a.res_scale, h[c].y, y[c].y * behind[c].y),
+                           fmaf(a.res_scale, h[c].z, y[c].z * behind[c].z),
+                           fmaf(a.res_scale, h[c].w, y[c].w * behind[c].w));
+        if (tid + 64 * WAVES * c < n4) store4(a.h_out + row * a.h_out_ld + at[c], h[c]);
       }
     }
-  }
-  if constexpr (!std::is_same_v<Out, Absent>) {
-    normalise<WAVES, CHUNKS>(h, a.pre, tid, n4, H, a.eps, a.pre_weight, part + 2);
+    if constexpr (HAS_OUT) {
+      normalise<WAVES, CHUNKS>(h, a.pre, tid, n4, H, a.eps, part[parity] + 2);
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-      const int i = tid + 64 * WAVES * c;
-      if (i < n4) {
-        float4 z = h[c];
-        if (a.scale) {
-          const float4 m = load4(a.scale + mod * a.hidden + 4 * i);
-          z = mul4(z, make_float4(1.f + m.x, 1.f + m.y, 1.f + m.z, 1.f + m.w));
-        }
-        if (a.shift) {
-          const float4 m = load4(a.shift + mod * a.hidden + 4 * i);
-          z = make_float4(z.x + m.x, z.y + m.y, z.z + m.z, z.w + m.w);
-        }
-        store4((Out*)a.out + row * a.out_ld + 4 * i, z);
-      }
+      for (int c = 0; c < CHUNKS; ++c)
+        if (tid + 64 * WAVES * c < n4)
+          store4((Out*)a.out + row * a.out_ld + at[c],
+                 make_float4(fmaf(h[c].x, before[c].x, shift[c].x),
+                             fmaf(h[c].y, before[c].y, shift[c].y),
+                             fmaf(h[c].z, before[c].z, shift[c].z),
+                             fmaf(h[c].w, before[c].w, shift[c].w)));
     }
   }
 }
@@ -160,17 +224,27 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(NormArgs a) {
 template <typename Y, typename Out>
 hipError_t launch(const NormArgs& a, hipStream_t s) {
   const int n4 = a.hidden / 4;
-#define RN(W, C)                                                                            \
-  hipLaunchKernelGGL((residual_norm_kernel<W, C, Y, Out>),                                  \
-                     dim3((unsigned)((a.rows + 4 / W - 1) / (4 / W))), dim3(256), 0, s, a)
+  // Runs of up to four rows, of fewer where four would leave less than 1024
+  // waves.  32760 rows of 1536 with 1 / 2 / 3 / 4 / 6 / 8 rows each: 145 / 125 /
+  // 119 / 119 / 122 / 125 us; 8000 of 4096: 137 / 100 / 95 / 87 / 89 / 86; 1000 of
+  // 1024 (fp32, 2 / 3 / 4 / 8): 9.9 / 9.7 / 10.5 / 13.1.
+#define RN(W, C)                                                                               \
+  do {                                                                                         \
+    const int64_t most = a.rows / (1024 / W);                                                  \
+    const int per = most < 1 ? 1 : most > 4 ? 4 : (int)most;                                   \
+    hipLaunchKernelGGL((residual_norm_kernel<W, C, Y, Out>),                                   \
+                       dim3((unsigned)((a.rows + per - 1) / per)), dim3(64 * W), 0, s, a, per); \
+  } while (0)
   if (n4 <= 64) RN(1, 1);
   else if (n4 <= 128) RN(1, 2);
-  else if (n4 <= 256) RN(1, 4);
-  else if (n4 <= 384) RN(1, 6);
-  else if (n4 <= 512) RN(1, 8);
+  else if (n4 <= 192) RN(1, 3);
+  else if (n4 <= 256) RN(2, 2);
+  else if (n4 <= 384) RN(2, 3);
+  else if (n4 <= 512) RN(4, 2);
+  else if (n4 <= 768) RN(4, 3);
   else if (n4 <= 1024) RN(4, 4);
-  else if (n4 <= 2048) RN(4, 8);
-  else RN(4, 16);
+  else if (n4 <= 1536) RN(8, 3);
+  else RN(8, 4);
 #undef RN
   return hipGetLastError();
 }
@@ -192,8 +266,8 @@ extern "C" acid_status acid_residual_norm(const acid_residual_norm_args* n, int6
                                           int32_t hidden, hipStream_t stream) {
   if (!n) return set_error(ACID_ERR_INVALID_ARG, "residual norm args NULL");
   if (rows < 0) return set_error(ACID_ERR_INVALID_ARG, "rows < 0");
-  if (hidden < 4 || hidden % 4 || hidden > 16384)
-    return set_error(ACID_ERR_SHAPE, "hidden %d: multiple of 4 in [4, 16384]", hidden);
+  if (hidden < 4 || hidden % 4 || hidden > 8192)
+    return set_error(ACID_ERR_SHAPE, "hidden %d: multiple of 4 in [4, 8192]", hidden);
   if (rows > (int64_t)1 << 23)
     return set_error(ACID_ERR_SHAPE, "rows %lld: at most 2^23", (long long)rows);
   for (int kind : {n->post, n->pre})

@@ -96,7 +96,7 @@ def _norm(lib, rows=10, hidden=256, **kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(rows=-1), BAD), (dict(hidden=0), SHAPE), (dict(hidden=258), SHAPE),
-    (dict(hidden=16388), SHAPE), (dict(rows=(1 << 23) + 1), SHAPE), (dict(post=3), BAD),
+    (dict(hidden=8196), SHAPE), (dict(rows=(1 << 23) + 1), SHAPE), (dict(post=3), BAD),
     (dict(pre=-1), BAD), (dict(y_dtype=5), BAD), (dict(out_dtype=5), BAD), (dict(eps=-1e-6), BAD),
     (dict(eps=float("nan")), BAD), (dict(eps=float("inf")), BAD),
     (dict(res_scale=float("inf")), BAD), (dict(rows_per_mod=-1), BAD), (dict(h=None), BAD),
