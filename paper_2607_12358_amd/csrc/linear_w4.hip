@@ -38,15 +38,15 @@ __device__ __forceinline__ bf16x8 load_x(const bf16* p, int) {
 }
 __device__ __forceinline__ bf16x8 load_x(const float* p, int part) {
   const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+  const uint32_t less0 = part > 0 ? 0xffff0000u : 0u, less1 = part > 1 ? 0xffff0000u : 0u;
   uint32_t u[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float v = i < 4 ? a[i & 3] : b[i & 3];
-    const float p0 = __uint_as_float(__float_as_uint(v) & 0xffff0000u), r = v - p0;
-    const float p1 = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-    u[i] = __float_as_uint(part == 0 ? p0 : part == 1 ? p1 : r - p1);
+    const float r = v - __uint_as_float(__float_as_uint(v) & less0);
+    u[i] = __float_as_uint(r - __uint_as_float(__float_as_uint(r) & less1));
   }
-  u32x4 out;
+  u32x4 out;  // the upper halves
 #pragma unroll
   for (int i = 0; i < 4; ++i) out[i] = __builtin_amdgcn_perm(u[2 * i + 1], u[2 * i], 0x07060302u);
   return __builtin_bit_cast(bf16x8, out);
@@ -62,13 +62,18 @@ struct W4Args {
   int32_t M, N, K, gelu;
 };
 
+// Sixteen waves pay where few tiles meet many blocks: 1536 x 8960, one row, 6.4 ->
+// 5.6 us (of 1536 inputs, twelve waves to eight: 3.7 -> 4.1).
+template <int NT, int MT>
+constexpr int MOST_WAVES = NT * MT == 1 ? 16 : 8;
+
 // A workgroup owns NT tiles of outputs and MT tiles of operand rows; its
 // waves take the 128-input blocks in turn and their sums are added in wave
 // order.  The matrix products give sum x (16 + c); one more product with the
 // constant -24, shared by the output tiles, makes that sum x (c - 8) before
 // the group's scale.
 template <typename X, typename Out, int GROUP, int NT, int MT>
-__global__ __launch_bounds__(512) void linear_w4_kernel(W4Args a) {
+__global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4Args a) {
   constexpr int RPT = std::is_same_v<X, float> ? 5 : 16;  // rows of a row tile
   extern __shared__ float red[];                          // [wave][mt][nt][16][16]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
@@ -102,36 +107,55 @@ __global__ __launch_bounds__(512) void linear_w4_kernel(W4Args a) {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  // a block's codes and scales, one block ahead of the products
+  u32x4 c_next[NT];
+  float s_next[NT][128 / GROUP];
+  auto load = [&](int b) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      c_next[nt] = codes[nt][b * 64];
+#pragma unroll
+      for (int i = 0; i < 128 / GROUP; ++i)
+        s_next[nt][i] = scales[nt][(b * (128 / GROUP) + i) * 16];
+    }
+  };
+  load(wave);  // there are no more waves than blocks
   for (int b = wave; b < KB; b += waves) {
+    bf16x8 xf[MT][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) xf[mt][j] = load_x(x[mt] + b * 128 + 32 * j, part);
     u32x4 c[NT];
     float s[NT][128 / GROUP];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      c[nt] = codes[nt][b * 64];
+      c[nt] = c_next[nt];
 #pragma unroll
-      for (int i = 0; i < 128 / GROUP; ++i) s[nt][i] = scales[nt][(b * (128 / GROUP) + i) * 16];
+      for (int i = 0; i < 128 / GROUP; ++i) s[nt][i] = s_next[nt][i];
     }
+    if (b + waves < KB) load(b + waves);
     f32x4 off[MT], sum[MT][NT];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool first = j * 32 % GROUP == 0, last = (j + 1) * 32 % GROUP == 0;
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const bf16x8 xf = load_x(x[mt] + b * 128 + 32 * j, part);
+      for (int mt = 0; mt < MT; ++mt)
         off[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            xf, minus24, first ? f32x4{0.f, 0.f, 0.f, 0.f} : off[mt], 0, 0, 0);
+            xf[mt][j], minus24, first ? f32x4{0.f, 0.f, 0.f, 0.f} : off[mt], 0, 0, 0);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+      for (int nt = 0; nt < NT; ++nt) {
+        const bf16x8 w = decode(c[nt][j]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
           sum[mt][nt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              xf, decode(c[nt][j]), first ? f32x4{0.f, 0.f, 0.f, 0.f} : sum[mt][nt], 0, 0, 0);
-        }
-        if (last) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+              xf[mt][j], w, first ? f32x4{0.f, 0.f, 0.f, 0.f} : sum[mt][nt], 0, 0, 0);
+          if (last) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               acc[mt][nt][i] =
                   fmaf(s[nt][j * 32 / GROUP], sum[mt][nt][i] + off[mt][i], acc[mt][nt][i]);
+          }
         }
       }
     }
@@ -149,6 +173,7 @@ __global__ __launch_bounds__(512) void linear_w4_kernel(W4Args a) {
     const int n = (tile0 + nt) * 16 + c, m = m0 + mt * RPT + r;
     if (n >= a.N || m >= a.M) continue;
     float y = 0.f;
+#pragma unroll 4
     for (int w = 0; w < waves; ++w) {
       const float* p = red + ((w * MT + mt) * NT + nt) * 256 + c;
       if constexpr (std::is_same_v<X, float>)
@@ -170,16 +195,28 @@ template <typename X, typename Out, int GROUP>
 hipError_t launch(const W4Args& a, hipStream_t s) {
   constexpr int RPT = std::is_same_v<X, float> ? 5 : 16;
   const int tiles = (a.N + 15) / 16, KB = a.K / 128;
-  const int waves = KB < 8 ? KB : 8;
 #define W4(NT, MT)                                                                            \
-  hipLaunchKernelGGL((linear_w4_kernel<X, Out, GROUP, NT, MT>),                               \
-                     dim3((tiles + NT - 1) / NT, (a.M + MT * RPT - 1) / (MT * RPT)),          \
-                     dim3(64 * waves), waves * NT * MT * 1024, s, a)
+  do {                                                                                        \
+    const int waves = KB < 8 ? KB : KB < 32 ? 8 : MOST_WAVES<NT, MT>;                         \
+    hipLaunchKernelGGL((linear_w4_kernel<X, Out, GROUP, NT, MT>),                             \
+                       dim3((tiles + NT - 1) / NT, (a.M + MT * RPT - 1) / (MT * RPT)),        \
+                       dim3(64 * waves), waves * NT * MT * 1024, s, a);                       \
+  } while (0)
+  // Two row tiles at once where there are two, so that codes are read and
+  // decoded once for both.  Output tiles: as many as leave a workgroup for each
+  // CU, since each reads the rows (4 KB a block and row tile, to 1 KB of codes
+  // an output tile).  28672 x 8192, bf16 rows, 1 / 16 / 32 of them: 27 / 31 / 45 us
+  // with four output tiles; 8192 x 28672: 30 / 58 / 72 with one (two of 32), 30 /
+  // 35 / 61 with two (four of 32).  Four row tiles ran slower than two and two.
+  const int most = tiles * ((a.M + 2 * RPT - 1) / (2 * RPT)) / 256;
   if (a.M <= RPT) {
-    if (tiles < 1024) W4(1, 1);
-    else W4(4, 1);
+    if (most >= 4) W4(4, 1);
+    else if (most >= 2) W4(2, 1);
+    else W4(1, 1);
   } else {
-    W4(2, 2);
+    if (most >= 4) W4(4, 2);
+    else if (most >= 2) W4(2, 2);
+    else W4(1, 2);
   }
 #undef W4
   return hipGetLastError();
