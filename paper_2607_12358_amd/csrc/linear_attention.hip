@@ -452,7 +452,7 @@ __device__ __forceinline__ void add_outer(State<D>& s, uint32_t columns, const V
       const Operand<T> a = column_operand<D>(columns, 16 * kt, 32 * ks * Rows<T, D>::BYTES, T());
 #pragma unroll
       for (int p = PARTS - 1; p >= 0; --p) s.t[kt] = mma(a, b[p], s.t[kt]);
-      if (kt % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      if (D == 128 && kt % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // registers
     }
   }
 }
@@ -697,13 +697,12 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
   for (int tt = 0; tt < 4; ++tt) tile_decay[tt] = uniform(a.scale * exp2_fast(-rate * (float)(16 * tt)));
   // the scores' tiles of this wave, 4 tq + st a digit: tokens 16 tq .., keys 16
   // st ..; the ten on and below the diagonal, and the two beside an even
-  // diagonal one, which are written as zeros
+  // diagonal one, which come out as zeros
   const uint32_t tiles =
-      D == 64 ? (wave == 0 ? 0xf10 : wave == 1 ? 0xe54 : wave == 2 ? 0xba98 : 0xdc)
+      D == 64    ? (wave == 0 ? 0xf10 : wave == 1 ? 0xe54 : wave == 2 ? 0xa98 : 0xbdc)
       : wave < 4 ? (wave == 0 ? 0x10 : wave == 1 ? 0x54 : wave == 2 ? 0x8 : 0x9)
                  : (wave == 4 ? 0xba : wave == 5 ? 0xdc : wave == 6 ? 0xe : 0xf);
-  const int n_tiles = D == 64 ? (wave == 2 ? 4 : wave == 3 ? 2 : 3)
-                              : (wave < 2 || wave == 4 || wave == 5 ? 2 : 1);
+  const int n_tiles = D == 64 ? 3 : wave < 2 || wave == 4 || wave == 5 ? 2 : 1;
   __builtin_amdgcn_s_waitcnt(0);  // S is here: no wait for it among the chunks' loads
   int64_t c0 = begin;
   // One chunk of n tokens: 64, or (WHOLE false) a sequence's last ones.
@@ -716,10 +715,11 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     if (!WHOLE) v.mask(n, lane);
 
     const uint32_t along = afresh(buf + R::at(col, 4 * g));
+#pragma unroll(D == 64 ? 3 : 1)
     for (int i = 0; i < n_tiles; ++i) {
       const int tq = tiles >> (4 * i + 2) & 3, st = tiles >> (4 * i) & 3;
       f32x4 p = {0.f, 0.f, 0.f, 0.f};
-      if (st <= tq) {
+      if (D == 64 || st <= tq) {
         const uint32_t k_at = (along ^ R::tile_bits(st)) + R::TOTAL + 16 * st * R::BYTES;
         const uint32_t q_at = (along ^ R::tile_bits(tq)) + 16 * tq * R::BYTES;
 #pragma unroll
@@ -727,7 +727,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
           p = mma(split_operand<D>(k_at, 32 * kk, 0, T()), split_operand<D>(q_at, 32 * kk, 0, T()), p);
       }
       const int far = 16 * (tq - st) + col - 4 * g;  // from the lane's first key
-      if (st < tq) {
+      if (D == 128 && st < tq) {
         const float w = a.scale * exp2_fast(-rate * (float)(far - 3));
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] *= w * pw.p[4 + i];
@@ -751,7 +751,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
 #pragma unroll
         for (int p = TWO - 1; p >= 0; --p) out[tt] = mma(sf[p], qf, out[tt]);
       }
-      __builtin_amdgcn_sched_barrier(0);
+      if (D == 128) __builtin_amdgcn_sched_barrier(0);  // registers
     }
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) out[tt] *= exp2_fast(-rate * (float)(col + 1)) * tile_decay[tt];
@@ -768,7 +768,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
                         score_operand(weights ^ P::tile_bits(tt), 32 * ks,
                                             16 * tt * P::BYTES + p * P::TOTAL, T()),
                         out[tt]);
-    __builtin_amdgcn_sched_barrier(0);
+    if (D == 128) __builtin_amdgcn_sched_barrier(0);
     T* at = o + c0 * o_ld + col * o_ld + 4 * g;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
@@ -818,20 +818,27 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_chunk_kernel
     chunks_of<T, D, true>(a, rows, seg, hs, len, begin, len);
 }
 
-// Tokens of a segment, a multiple of 64, and how many there are.  One segment
-// a head once the heads alone give every CU its two workgroups; else as many
-// as fill them in one round.
+// Tokens of a segment, a multiple of 64, and how many there are: as many as
+// give each CU a workgroup, or two where they then have eight chunks each (one
+// segment a head once the heads alone do).  With 256 / 512 workgroups: 12 x 4680
+// tokens (d = 128) 44 / 49 us, 1 x 30000 43 / 61, 4 x 8192 (d = 64) 24 / 30, but 12
+// x 32760 178 / 171.
 struct Segments {
   int64_t tokens, count;
 };
 Segments segments_of(int64_t heads, int64_t L) {
-  const int64_t chunks = (L + kChunk - 1) / kChunk, slots = 2 * 256;
-  int64_t most = heads > 0 ? slots / heads : 1;
-  if (most < 1) most = 1;
-  const int64_t per = chunks > most ? (chunks + most - 1) / most : 1;
-  if (chunks <= 1 || most == 1) return {chunks * kChunk, 1};
+  const int64_t chunks = (L + kChunk - 1) / kChunk;
+  const int64_t groups = heads * chunks >= 512 * 8 ? 512 : 256;
+  const int64_t most = heads > 0 ? groups / heads : 1;
+  if (chunks <= 1 || most <= 1) return {chunks * kChunk, 1};
+  const int64_t per = (chunks + most - 1) / most;
   return {per * kChunk, (chunks + per - 1) / per};
 }
+
+// Up to this many segments the outputs' kernel adds those before its own
+// itself; more take a scan, a launch of its own (4 segments, d = 128: 16.9 us
+// for 18.5; 13: 30.9 for 28.6; 25, d = 64: 21.7 for 18.9).
+constexpr int64_t kFolded = 8;
 
 template <typename T, int D>
 hipError_t launch_chunks(const ChunkArgs& a, int64_t heads, hipStream_t s) {
@@ -932,7 +939,8 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
   ACID_TRY(on.enter(stream));
   const ChunkArgs a = {q_dev, k_dev, vt_dev, o_dev, vt_ld, slopes_dev, lengths_dev, state_in_dev,
                        state_out_dev, seg.count > 1 ? (float*)workspace_dev : nullptr, seq_len,
-                       n_heads, (int32_t)seg.count, (int32_t)seg.tokens, seg.count > 8, scale};
+                       n_heads, (int32_t)seg.count, (int32_t)seg.tokens,
+                       seg.count > kFolded, scale};
   hipError_t e;
   if (dtype == ACID_BF16)
     e = head_dim == 64 ? launch_chunks<bf16, 64>(a, heads, stream)
