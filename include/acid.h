@@ -460,8 +460,9 @@ acid_status acid_block_forward(acid_model* m, int32_t block,
  *   S_t = lambda S_{t-1} + k_t^T v_t   (S_{-1}: state_in, or 0 if NULL)
  *   o_t = scale q_t S_t
  * q, k: [n_seq][n_heads][L][d]; vt: V transposed, [n_seq][n_heads][d][vt_ld]
- * with vt_ld >= round_up(L, 8), a multiple of 8 (the layout the QKV epilogue
- * writes and acid_attention reads); o: [n_seq][L][n_heads*d]; all in `dtype`.
+ * with vt_ld >= round_up(L, 8), a multiple of 8, <= 2^28 (the layout the QKV
+ * epilogue writes and acid_attention reads); o: [n_seq][L][n_heads*d]; all in
+ * `dtype`.
  * States: fp32 [n_seq][n_heads][d][d], row i over k's column i; state_out
  * (NULL: not wanted) may be state_in itself.  lengths_dev (NULL: all L):
  * sequence b has lengths[b] tokens, clamped to [0, L]; what the padding holds

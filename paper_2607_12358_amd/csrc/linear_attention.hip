@@ -147,7 +147,7 @@ hipError_t launch_step(int dtype, int d, const StepArgs& a, hipStream_t s) {
 // chunks that follow; where it is summed to an fp32 state that is returned, or
 // carried to another segment, V goes in as three parts, which is exact.
 constexpr int kChunk = 64;
-constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 64;
+constexpr int64_t kMaxTokens = (int64_t)1 << 28;
 
 template <typename T>
 struct Operand;  // eight values of the contracted index
@@ -229,6 +229,9 @@ __device__ __forceinline__ void dma16(uint64_t base, uint32_t off_bytes, uint32_
 __device__ __forceinline__ void barrier_all() {  // loads into LDS included
   __builtin_amdgcn_s_waitcnt(0);
   asm volatile("s_barrier" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 }
 __device__ __forceinline__ void barrier_lds() {
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -348,23 +351,33 @@ struct State {
   f32x4 t[D / 16];
 };
 
-// A wave's 16 columns of V for 64 tokens, as they are an operand: vt's rows,
-// tokens 32 ks + 8 g .. + 7 in lane g.
-template <typename T>
+// A wave's 16 columns of V for 64 tokens, vt's rows, by way of a part of LDS
+// that is this wave's alone: loaded there as whole rows (in registers' order,
+// 64 bytes of 16 rows at a time, a vt_ld that is no multiple of 128 bytes cost
+// 13% of the whole call), read as the operand they are, tokens 32 ks + 8 g .. + 7
+// in lane g.
+template <typename T, int D>
 struct ValueTile {
+  typedef Rows<T, kChunk, true> R;
+  static constexpr int BYTES = 16 * R::BYTES;  // of a wave
   Operand<T> v[2];
-  // at: the lane's row, at token c0 + 8 g
-  __device__ __forceinline__ void load(const T* at, int64_t c0, int64_t len, int lane) {
-    if (c0 + kChunk <= len) {
+  // at: vt's first row of the wave, at token c0, of which n follow
+  static __device__ __forceinline__ void load(const T* at, int64_t vt_ld, int n, uint32_t lds,
+                                              int lane) {
+    constexpr int SLOTS = R::BYTES / 16, ROWS = 64 / SLOTS;
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) v[ks] = load8(at + 32 * ks);
-    } else {  // eights from len on: the chunk's first one instead, to be masked
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const int g8 = 8 * (lane >> 4);
-        v[ks] = load8(at + (c0 + 32 * ks + g8 < len ? 32 * ks : -g8));
-      }
+    for (int i = 0; i < 16 / ROWS; ++i) {
+      const int r = lane / SLOTS, c = lane % SLOTS ^ R::swizzle(ROWS * i + r);
+      const int t = c * R::CHUNK < n ? c * R::CHUNK : 0;  // what is past the end is masked
+      dma16(uniform_ptr(at + (int64_t)(ROWS * i) * vt_ld),
+            (uint32_t)r * (uint32_t)(vt_ld * sizeof(T)) + (uint32_t)(t * sizeof(T)),
+            lds + i * 1024);
     }
+  }
+  __device__ __forceinline__ void read(uint32_t lds, int lane) {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+      v[ks] = score_operand(lds + R::at(lane & 15, 8 * (lane >> 4)), 32 * ks, 0, T());
   }
   // tokens from n on become zeros
   __device__ __forceinline__ void mask(int n, int lane) {
@@ -431,7 +444,7 @@ __device__ __forceinline__ void decayed(const Operand<float>& v, const float (&w
 // S += K^T (decayed V) over 64 tokens; token t decays over last - t, last >= 63
 // if WHOLE.  columns: K's tile plus column_base().
 template <typename T, int D, int PARTS, bool WHOLE>
-__device__ __forceinline__ void add_outer(State<D>& s, uint32_t columns, const ValueTile<T>& v,
+__device__ __forceinline__ void add_outer(State<D>& s, uint32_t columns, const ValueTile<T, D>& v,
                                           float rate, const Powers& pw, int last, int lane) {
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) {
@@ -448,11 +461,16 @@ __device__ __forceinline__ void add_outer(State<D>& s, uint32_t columns, const V
     Operand<T> b[PARTS];
     decayed(v.v[ks], w, b);
 #pragma unroll
-    for (int kt = 0; kt < D / 16; ++kt) {
-      const Operand<T> a = column_operand<D>(columns, 16 * kt, 32 * ks * Rows<T, D>::BYTES, T());
+    for (int k0 = 0; k0 < D / 16; k0 += 4) {  // products on one accumulator stay apart
+      Operand<T> a[4];
 #pragma unroll
-      for (int p = PARTS - 1; p >= 0; --p) s.t[kt] = mma(a, b[p], s.t[kt]);
-      if (D == 128 && kt % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // registers
+      for (int k = 0; k < 4; ++k)
+        a[k] = column_operand<D>(columns, 16 * (k0 + k), 32 * ks * Rows<T, D>::BYTES, T());
+#pragma unroll
+      for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s.t[k0 + k] = mma(a[k], b[p], s.t[k0 + k]);
+      if (D == 128) __builtin_amdgcn_sched_barrier(0);  // registers
     }
   }
 }
@@ -511,7 +529,8 @@ __device__ __forceinline__ void write_state(State<D>& s, float* p) {
 template <typename T, int D>
 __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_state_kernel(ChunkArgs a) {
   typedef Rows<T, D> R;
-  __shared__ __align__(1024) unsigned char rows[2 * R::TOTAL];
+  typedef ValueTile<T, D> V;
+  __shared__ __align__(1024) unsigned char rows[2 * R::TOTAL + 2 * (D / 16) * V::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int seg = blockIdx.x % (a.segments - 1);
   const int64_t hs = blockIdx.x / (a.segments - 1);  // sequence and head
@@ -535,25 +554,27 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_state_kernel
     for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{0.f, 0.f, 0.f, 0.f}; });
   }
   const T* k = (const T*)a.k + hs * a.tokens * D;
-  const T* vt = (const T*)a.vt + (hs * D + wave * 16 + (lane & 15)) * a.vt_ld + 8 * (lane >> 4);
-  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void_t*)rows;
-  ValueTile<T> v, v_next;
-  load_rows<T, D>(uniform_ptr(k + begin * D), kChunk, lds, wave, lane);
-  v.load(vt + begin, begin, len, lane);
-  uint32_t buf = lds, next = lds + R::TOTAL;
-  __builtin_amdgcn_s_waitcnt(0);
+  const T* vt = (const T*)a.vt + (hs * D + wave * 16) * a.vt_ld;
+  uint32_t buf = (uint32_t)(uintptr_t)(lds_void_t*)rows, next = buf + R::TOTAL;
+  uint32_t v_buf = buf + 2 * R::TOTAL + wave * (2 * V::BYTES), v_next = v_buf + V::BYTES;
+  load_rows<T, D>(uniform_ptr(k + begin * D), kChunk, buf, wave, lane);
+  V::load(vt + begin, a.vt_ld, kChunk, v_buf, lane);
   for (int64_t c0 = begin; c0 < end; c0 += kChunk) {
     barrier_all();
     if (c0 + kChunk < end) {
       load_rows<T, D>(uniform_ptr(k + (c0 + kChunk) * D), kChunk, next, wave, lane);
-      v_next.load(vt + c0 + kChunk, c0 + kChunk, len, lane);
+      V::load(vt + c0 + kChunk, a.vt_ld, kChunk, v_next, lane);
     }
+    V v;
+    v.read(v_buf, lane);
     add_outer<T, D, PARTS, true>(s, afresh(buf + column_base<T, D>(lane)), v, rate, pw,
                                  (int)(end - 1 - c0), lane);
-    v = v_next;
-    const uint32_t t = buf;
+    uint32_t t = buf;
     buf = next;
     next = t;
+    t = v_buf;
+    v_buf = v_next;
+    v_next = t;
   }
   for_state(s, [&](f32x4& t, int at, int, int) {
     *reinterpret_cast<f32x4*>(slot + D * D + at) = t;
@@ -647,8 +668,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
 
   const T* q = (const T*)a.q + hs * a.tokens * D;
   const T* k = (const T*)a.k + hs * a.tokens * D;
-  const T* vt = (const T*)a.vt + (hs * D + wave * 16 + (threadIdx.x & 15)) * a.vt_ld +
-                8 * ((threadIdx.x & 63) >> 4);
+  const T* vt = (const T*)a.vt + (hs * D + wave * 16) * a.vt_ld;
   const int64_t o_ld = (int64_t)a.heads * D;
   T* o = (T*)a.o + seq * a.tokens * o_ld + head * D + wave * 16;
   // lambda^64, for a state in fp32 in two parts: a rounded factor would add up
@@ -658,16 +678,28 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
   const Powers pw(rate);
   const float whole_hi = uniform((float)whole);
   const float whole_lo = uniform((float)(whole - (double)whole_hi));
-  uint32_t buf = (uint32_t)(uintptr_t)(lds_void_t*)rows, next = buf + 2 * R::TOTAL;
-  const uint32_t scores = buf + 4 * R::TOTAL;
-  ValueTile<T> v, v_next;
-  auto load = [&](int64_t c0, uint32_t to, ValueTile<T>& values, int lane) {
-    const int n = end - c0 < kChunk ? (int)(end - c0) : kChunk;
-    load_rows<T, D>(uniform_ptr(q + c0 * D), n, to, wave, lane);
-    load_rows<T, D>(uniform_ptr(k + c0 * D), n, to + R::TOTAL, wave, lane);
-    values.load(vt + c0, c0, len, lane);
+  // LDS: K's rows of this chunk and the next, Q's, V's (each wave its own),
+  // the scores.  Q and V have one place each: the next chunk's are loaded once
+  // all that is in it has been read.
+  typedef ValueTile<T, D> V;
+  uint32_t buf = (uint32_t)(uintptr_t)(lds_void_t*)rows, next = buf + R::TOTAL;
+  const uint32_t q_at = buf + 2 * R::TOTAL, v_at = q_at + R::TOTAL + wave * V::BYTES;
+  const uint32_t scores = q_at + R::TOTAL + (D / 16) * V::BYTES;
+  V v;
+  auto tokens = [&](int64_t c0) { return end - c0 < kChunk ? (int)(end - c0) : kChunk; };
+  auto load_k = [&](int64_t c0, uint32_t to, int lane) {
+    load_rows<T, D>(uniform_ptr(k + c0 * D), tokens(c0), to, wave, lane);
   };
-  if (begin < end) load(begin, buf, v, threadIdx.x & 63);
+  auto load_q = [&](int64_t c0, int lane) {
+    load_rows<T, D>(uniform_ptr(q + c0 * D), tokens(c0), q_at, wave, lane);
+  };
+  auto load_v = [&](int64_t c0, int lane) { V::load(vt + c0, a.vt_ld, tokens(c0), v_at, lane); };
+  if (begin < end) {
+    const int lane = threadIdx.x & 63;
+    load_k(begin, buf, lane);
+    load_q(begin, lane);
+    load_v(begin, lane);
+  }
 
   State<D> s;
   if (seg == 0) {
@@ -711,20 +743,20 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     // made afresh in each chunk: what follows from it is more than registers hold
     const int lane = (int)afresh(threadIdx.x & 63), col = lane & 15, g = lane >> 4;
     barrier_all();
-    if (c0 + kChunk < end) load(c0 + kChunk, next, v_next, lane);
-    if (!WHOLE) v.mask(n, lane);
-
-    const uint32_t along = afresh(buf + R::at(col, 4 * g));
+    const bool more = c0 + kChunk < end;
+    if (more) load_k(c0 + kChunk, next, lane);
+    v.read(v_at, lane);
+    const uint32_t along = afresh(R::at(col, 4 * g));
 #pragma unroll(D == 64 ? 3 : 1)
     for (int i = 0; i < n_tiles; ++i) {
       const int tq = tiles >> (4 * i + 2) & 3, st = tiles >> (4 * i) & 3;
       f32x4 p = {0.f, 0.f, 0.f, 0.f};
       if (D == 64 || st <= tq) {
-        const uint32_t k_at = (along ^ R::tile_bits(st)) + R::TOTAL + 16 * st * R::BYTES;
-        const uint32_t q_at = (along ^ R::tile_bits(tq)) + 16 * tq * R::BYTES;
+        const uint32_t k_tile = (along ^ R::tile_bits(st)) + buf + 16 * st * R::BYTES;
+        const uint32_t q_tile = (along ^ R::tile_bits(tq)) + q_at + 16 * tq * R::BYTES;
 #pragma unroll
         for (int kk = 0; kk < D / 32; ++kk)
-          p = mma(split_operand<D>(k_at, 32 * kk, 0, T()), split_operand<D>(q_at, 32 * kk, 0, T()), p);
+          p = mma(split_operand<D>(k_tile, 32 * kk, 0, T()), split_operand<D>(q_tile, 32 * kk, 0, T()), p);
       }
       const int far = 16 * (tq - st) + col - 4 * g;  // from the lane's first key
       if (D == 128 && st < tq) {
@@ -738,6 +770,11 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
       }
       store_scores(scores + P::at(16 * tq + col, 16 * st + 4 * g), P::TOTAL, p, T());
     }
+    if (more) {
+      wait_lds();  // v is in its registers
+      load_v(c0 + kChunk, lane);
+    }
+    if (!WHOLE) v.mask(n, lane);
     f32x4 out[4];
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) out[tt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -745,28 +782,31 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     for (int kk = 0; kk < D / 32; ++kk) {
       Operand<T> sf[TWO];
       state_operand(s, kk, sf);
+      Operand<T> qf[4];
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt) {
-        const Operand<T> qf = split_operand<D>(along ^ R::tile_bits(tt), 32 * kk, 16 * tt * R::BYTES, T());
+      for (int tt = 0; tt < 4; ++tt)
+        qf[tt] = split_operand<D>((along ^ R::tile_bits(tt)) + q_at, 32 * kk, 16 * tt * R::BYTES, T());
 #pragma unroll
-        for (int p = TWO - 1; p >= 0; --p) out[tt] = mma(sf[p], qf, out[tt]);
-      }
+      for (int p = TWO - 1; p >= 0; --p)
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) out[tt] = mma(sf[p], qf[tt], out[tt]);
       if (D == 128) __builtin_amdgcn_sched_barrier(0);  // registers
     }
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) out[tt] *= exp2_fast(-rate * (float)(col + 1)) * tile_decay[tt];
     barrier_lds();
+    if (more) load_q(c0 + kChunk, lane);
 
     const uint32_t weights = afresh(scores + P::at(col, 8 * g));
 #pragma unroll
-    for (int tt = 0; tt < 4; ++tt)
+    for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int ks = 0; ks <= tt / 2; ++ks)
+      for (int p = TWO - 1; p >= 0; --p)
 #pragma unroll
-        for (int p = TWO - 1; p >= 0; --p)
+        for (int tt = 2 * ks; tt < 4; ++tt)
           out[tt] = mma(v.v[ks],
                         score_operand(weights ^ P::tile_bits(tt), 32 * ks,
-                                            16 * tt * P::BYTES + p * P::TOTAL, T()),
+                                      16 * tt * P::BYTES + p * P::TOTAL, T()),
                         out[tt]);
     if (D == 128) __builtin_amdgcn_sched_barrier(0);
     T* at = o + c0 * o_ld + col * o_ld + 4 * g;
@@ -786,10 +826,9 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
         const float w = exp2_fast(-rate * (float)n);
         for_state(s, [&](f32x4& t, int, int, int) { t *= w; });
       }
-      add_outer<T, D, PARTS, WHOLE>(s, afresh(buf + R::TOTAL + column_base<T, D>(lane)), v, rate,
+      add_outer<T, D, PARTS, WHOLE>(s, afresh(buf + column_base<T, D>(lane)), v, rate,
                                     pw, n - 1, lane);
     }
-    v = v_next;
     const uint32_t t = buf;
     buf = next;
     next = t;
@@ -805,8 +844,8 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
 
 template <typename T, int D>
 __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_chunk_kernel(ChunkArgs a) {
-  // LDS: Q's and K's rows of one chunk, of the next one, the scores
-  __shared__ __align__(1024) unsigned char rows[4 * Rows<T, D>::TOTAL +
+  __shared__ __align__(1024) unsigned char rows[3 * Rows<T, D>::TOTAL +
+                                                (D / 16) * ValueTile<T, D>::BYTES +
                                                 (sizeof(T) == 2 ? 2 : 1) * Rows<T, kChunk>::TOTAL];
   const int seg = blockIdx.x % a.segments;
   const int64_t hs = blockIdx.x / a.segments;
@@ -894,10 +933,10 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
   ACID_TRY(check_heads(dtype, n_seq, n_heads, head_dim));
   if (seq_len < 0) return set_error(ACID_ERR_INVALID_ARG, "seq_len < 0");
   if (seq_len > kMaxTokens)
-    return set_error(ACID_ERR_SHAPE, "seq_len %lld: below 2^31 - 63", (long long)seq_len);
-  if (vt_ld < round_up(seq_len, 8) || vt_ld % 8 || vt_ld > ((int64_t)1 << 31))
+    return set_error(ACID_ERR_SHAPE, "seq_len %lld: at most 2^28", (long long)seq_len);
+  if (vt_ld < round_up(seq_len, 8) || vt_ld % 8 || vt_ld > ((int64_t)1 << 28))
     return set_error(ACID_ERR_SHAPE,
-                     "vt_ld %lld must be a multiple of 8, >= round_up(L, 8) and <= 2^31",
+                     "vt_ld %lld must be a multiple of 8, >= round_up(L, 8) and <= 2^28",
                      (long long)vt_ld);
   if (n_seq == 0) return ACID_OK;
   if (!slopes_dev || (seq_len > 0 && (!q_dev || !k_dev || !vt_dev || !o_dev)))
