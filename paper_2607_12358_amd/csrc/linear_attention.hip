@@ -3,7 +3,9 @@
 //
 //   S_t = lambda S_{t-1} + k_t^T v_t,  o_t = scale q_t S_t,  lambda = exp(-slope)
 //
-// S is fp32 [d][d] (rows over k's columns, columns over v's).
+// S is fp32 [d][d] (rows over k's columns, columns over v's).  Both forms move
+// little more than they must: a token costs 4 d^2 operations a head for 4 d
+// values, a single token reads and writes its states.
 #include <type_traits>
 
 #include "common.h"
@@ -36,8 +38,11 @@ __device__ __forceinline__ int64_t find_slot(const int32_t* __restrict__ slots, 
   return -1;
 }
 
-// One token a row.  A workgroup owns 32 columns of one head's state: thread
-// (rg, cg) holds rows rg + 32 i, columns 4 cg .. 4 cg + 3.
+// One token a row.  Bound by the states, read and written once: 256 rows of 12
+// heads (d = 128), 391 MB, take 81 us, 4.8 TB/s.  A workgroup owns 32 columns of
+// one head's state, so that one row of 12 heads still makes 48 of them (3.4 us):
+// thread (rg, cg) holds rows rg + 32 i, columns 4 cg .. 4 cg + 3, and the sums over
+// rows go over lanes, then over waves in LDS.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void la_step_kernel(StepArgs a) {
   constexpr int R = D / 32;
@@ -137,9 +142,20 @@ hipError_t launch_step(int dtype, int d, const StepArgs& a, hipStream_t s) {
 // formed transposed (rows: v's columns, columns: tokens), so that a lane
 // stores four neighbouring values.
 //
-// LDS holds what the waves share: Q's and K's rows, loaded there directly a
-// chunk ahead, and the masked scores.  K's operand of the outer products lies
-// across those rows; bf16 reads it with the transposing LDS load.
+// LDS holds what the waves share, Q's and K's rows and the masked scores, and
+// V's rows, each wave's its own; all are loaded there directly, a chunk ahead.
+// K's operand of the outer products lies across those rows; bf16 reads it with
+// the transposing LDS load.
+//
+// 12 heads of 32760 tokens (d = 128, bf16) take 166 us in three launches: the
+// segments' states 51 us (232 MB), the scan of them 12 (62 MB) and the outputs 99
+// (431 MB), 4.3 to 5.2 TB/s where a copy makes 5.0; K and V are read twice,
+// because a segment's outputs need the states of those before it.  The outputs'
+// kernel keeps its vector units busy for half of that time too (S and the
+// scores made into operands, V decayed), with 16 waves a CU to hide it: 80 KB
+// of LDS and 128 registers a lane are what two workgroups have.  One wave for
+// 32 columns, half as many waves, took 115 us.  vt_ld = 32760 itself costs 10%:
+// rows that are no multiple of 128 bytes apart take two lines for one.
 //
 // Rounding.  A bf16 operand made from fp32 values would cost the output half
 // of its accuracy, so scores and S go into their products as two bf16 parts
@@ -241,8 +257,8 @@ __device__ __forceinline__ void barrier_lds() {
 // c ^ swizzle(r).  With 64 banks of four bytes, all of these hit each bank
 // equally often: half chunks of 16 neighbouring rows (split_operand); two
 // neighbouring chunks of rows 8 g + 0 .. 3 (bf16 across the rows) or four of rows
-// 8 g (fp32 across the rows); whole chunks of 16 rows of scores (row_operand; of
-// bf16 rows of K and Q they would take two turns).
+// 8 g (fp32 across the rows); whole chunks of 16 rows of scores and of V
+// (score_operand; of bf16 rows of K and Q they would take two turns).
 //
 // Rows are a power of two long and the swizzle is linear in r's bits, so
 // at(r ^ r1, x ^ x1) == at(r, x) ^ at(r1, x1): a lane keeps one address and
@@ -352,10 +368,9 @@ struct State {
 };
 
 // A wave's 16 columns of V for 64 tokens, vt's rows, by way of a part of LDS
-// that is this wave's alone: loaded there as whole rows (in registers' order,
-// 64 bytes of 16 rows at a time, a vt_ld that is no multiple of 128 bytes cost
-// 13% of the whole call), read as the operand they are, tokens 32 ks + 8 g .. + 7
-// in lane g.
+// that is this wave's alone: loaded there as whole rows (straight into
+// registers, 64 bytes of 16 rows at a time, took 5% longer and eight registers
+// more), read as the operand they are, tokens 32 ks + 8 g .. + 7 in lane g.
 template <typename T, int D>
 struct ValueTile {
   typedef Rows<T, kChunk, true> R;

