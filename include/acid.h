@@ -491,7 +491,8 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
  * leaves the new one in that slot of state_out (state_in itself, or a buffer
  * apart, whose other slots are left as they are).  A slot outside [0, n_slots)
  * marks a padding row: nothing of it is read or written.  Rows with the same
- * slot are one sequence's successive tokens, in row order.  q, k, v, o: rows
+ * slot are one sequence's successive tokens, in row order; with slots at most
+ * 65536 rows, each of which looks through the others' slots.  q, k, v, o: rows
  * of n_heads*d in `dtype`, *_ld elements apart (whole 16 bytes): columns
  * h*d .. (h+1)*d belong to head h, as in a projection's Q | K | V. */
 acid_status acid_linear_attention_step(int32_t dtype, int64_t n_rows, int32_t n_heads,

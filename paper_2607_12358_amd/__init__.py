@@ -289,7 +289,7 @@ def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
     state fp32 [n_slots, heads, d, d], updated in place unless state_out is
     given; slots int32 [rows]: each row's state (default: its own index), any
     value outside [0, n_slots) marking a padding row that is left alone; rows
-    of one slot are successive tokens, in row order."""
+    of one slot are successive tokens, in row order (at most 65536 rows)."""
     torch = _torch()
     if state.dim() != 4:
         raise ValueError("state: expected [n_slots, heads, d, d]")

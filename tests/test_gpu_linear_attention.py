@@ -241,6 +241,27 @@ def test_step(dtype, rows, heads, d, n_slots, slots, in_place):
     assert (wide[:, :8] == 7.0).all() and (wide[:, 8 + w:] == 7.0).all()
 
 
+@pytest.mark.parametrize("rows", [1023, 1024, 1025, 5000])
+def test_slots_far_apart(rows):
+    """A slot's rows on both sides of the search's strides, among padding rows
+    that are left alone."""
+    P = need_gpu()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    where = {0: 5, 17: 9, 63: 2, 64: 2, 1022: 9, 1023: 5, 1024: 5, 1025: 2, 1041: 9, 2047: 3, 2048: 3,
+             2111: 3, 3100: 11, 4990: 9, 4999: 5}
+    slots = [where.get(r, -1) for r in range(rows)]
+    q, k, v = (torch.randn((rows, 64), generator=g, device="cuda") for _ in range(3))
+    slopes, state = torch.full((1,), 0.25, device="cuda"), torch.randn((16, 1, 64, 64), generator=g, device="cuda")
+    ro, rs, ao, as_ = _step_reference(*(_f64(x) for x in (q, k, v, slopes, state)), slots, 0.5, 16)
+    o = torch.full_like(q, 7.0)
+    P.linear_attention_step(q, k, v, slopes, o, state, scale=0.5,
+                            slots=torch.tensor(slots, dtype=torch.int32, device="cuda"))
+    acc = (64 + 16 + 5) * 2.0 ** -24
+    assert_elementwise(_f64(o), ro, acc * ao, 2.0 ** -24, "o")
+    assert_elementwise(_f64(state), rs, acc * as_, 0.0, "state")
+
+
 def test_steps_follow_a_prompt():
     """A prompt, then tokens one by one, against the whole sequence."""
     P = need_gpu()

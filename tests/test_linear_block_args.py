@@ -64,7 +64,7 @@ def _step(lib, **kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=2), BAD), (dict(rows=-1), BAD), (dict(heads=0), BAD), (dict(d=32), SHAPE),
     (dict(n_slots=-1), SHAPE), (dict(slots=None, n_slots=3), SHAPE),
-    (dict(n_slots=1 << 31), SHAPE), (dict(rows=1 << 22), SHAPE),
+    (dict(n_slots=1 << 31), SHAPE), (dict(rows=1 << 22), SHAPE), (dict(rows=65537), SHAPE),
     (dict(qld=120), SHAPE), (dict(kld=385), SHAPE), (dict(vld=1 << 33), SHAPE), (dict(old=64), SHAPE),
     (dict(q=None), BAD), (dict(k=None), BAD), (dict(v=None), BAD), (dict(o=None), BAD),
     (dict(slopes=None), BAD), (dict(sin=None), BAD), (dict(sout=None), BAD),
