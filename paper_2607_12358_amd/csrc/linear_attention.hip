@@ -285,18 +285,18 @@ template <typename T, int W, bool SCORES = false>
 struct Rows {
   static constexpr int BYTES = W * (int)sizeof(T), CHUNK = 16 / (int)sizeof(T);
   static constexpr int TOTAL = kChunk * BYTES;
-  static constexpr int swizzle(int r) {
-    const int b0 = r & 1, b1 = r >> 1 & 1, b2 = r >> 2 & 1, b3 = r >> 3 & 1, b4 = r >> 4 & 1;
+  static constexpr uint32_t swizzle(uint32_t r) {
+    const uint32_t b0 = r & 1, b1 = r >> 1 & 1, b2 = r >> 2 & 1, b3 = r >> 3 & 1, b4 = r >> 4 & 1;
     return sizeof(T) == 4 ? b0 | b1 << 1 | b3 << 2 | (b2 ^ b4) << 3
            : W == kChunk && SCORES ? b1 | b2 << 1 | b3 << 2
            : BYTES == 256 ? b2 | b0 << 1 | b1 << 2 | b3 << 3
                           : b2 | b1 << 1 | b3 << 2;  // 128 bytes: odd rows lie in the other banks
   }
-  static constexpr uint32_t at(int r, int x) {  // bytes
-    return (uint32_t)(r * BYTES + ((x / CHUNK ^ swizzle(r)) * 16) + x % CHUNK * (int)sizeof(T));
+  static constexpr uint32_t at(uint32_t r, uint32_t x) {  // bytes
+    return r * BYTES + (x / CHUNK ^ swizzle(r)) * 16 + x % CHUNK * (uint32_t)sizeof(T);
   }
   // what a step of 16 t rows, 16 t BYTES apart, flips besides
-  static constexpr uint32_t tile_bits(int t) { return (uint32_t)(swizzle(16 * t) * 16); }
+  static constexpr uint32_t tile_bits(uint32_t t) { return swizzle(16 * t) * 16; }
 };
 
 template <typename V>
@@ -316,15 +316,16 @@ __device__ __forceinline__ uint32_t afresh(uint32_t x) {
 // The tile of rows c0 .. c0 + n - 1 (base: row c0) into LDS, rows past it as
 // copies of the last one: sizeof(T) instructions of each of W / 16 waves.
 template <typename T, int W>
-__device__ __forceinline__ void load_rows(uint64_t base, int n, uint32_t lds, int wave, int lane) {
+__device__ __forceinline__ void load_rows(uint64_t base, int n, uint32_t lds, int wave,
+                                          uint32_t lane) {
   typedef Rows<T, W> R;
-  constexpr int SLOTS = W / R::CHUNK;
+  constexpr uint32_t SLOTS = W / R::CHUNK, ROWS = 64 / SLOTS;  // rows of an instruction
+  const uint32_t r = lane / SLOTS, c = (lane % SLOTS ^ R::swizzle(r)) * 16;
 #pragma unroll
   for (int i = 0; i < (int)sizeof(T); ++i) {
-    const int piece = (wave * (int)sizeof(T) + i) * 64 + lane;  // 16-byte piece of the tile
-    const int r = piece / SLOTS, c = piece % SLOTS ^ R::swizzle(r);
-    const int row = r < n ? r : n - 1;
-    dma16(base, (uint32_t)(row * R::BYTES + c * 16), lds + (wave * (int)sizeof(T) + i) * 1024);
+    const uint32_t piece = wave * (uint32_t)sizeof(T) + i, first = piece * ROWS;
+    const uint32_t row = first + r < (uint32_t)n ? first + r : (uint32_t)n - 1;
+    dma16(base, row * R::BYTES + (c ^ R::swizzle(first) * 16), lds + piece * 1024);
   }
 }
 
@@ -356,8 +357,8 @@ __device__ __forceinline__ Operand<float> split_operand(uint32_t base, int X, in
 // multiple of 16.  The transposing load hands the 16 lanes of a group the 16
 // columns of four rows of which each lane has addressed four values.
 template <typename T, int W>
-__device__ __forceinline__ uint32_t column_base(int lane) {
-  const int l = lane & 15, g = lane >> 4;
+__device__ __forceinline__ uint32_t column_base(uint32_t lane) {
+  const uint32_t l = lane & 15, g = lane >> 4;
   return sizeof(T) == 2 ? Rows<T, W>::at(8 * g + (l >> 2), 4 * (l & 3)) : Rows<T, W>::at(8 * g, l);
 }
 template <int W>
@@ -394,19 +395,20 @@ struct ValueTile {
   static constexpr int BYTES = 16 * R::BYTES;  // of a wave
   Operand<T> v[2];
   // at: vt's first row of the wave, at token c0, of which n follow
-  static __device__ __forceinline__ void load(const T* at, int64_t vt_ld, int n, uint32_t lds,
-                                              int lane) {
-    constexpr int SLOTS = R::BYTES / 16, ROWS = 64 / SLOTS;
+  static __device__ __forceinline__ void load(const T* at, int64_t vt_ld, uint32_t n,
+                                              uint32_t lds, uint32_t lane) {
+    constexpr uint32_t SLOTS = R::BYTES / 16, ROWS = 64 / SLOTS;  // rows of an instruction
+    const uint32_t r = lane / SLOTS, c = (lane % SLOTS ^ R::swizzle(r)) * 16;
+    const uint32_t row = r * (uint32_t)(vt_ld * sizeof(T));
 #pragma unroll
-    for (int i = 0; i < 16 / ROWS; ++i) {
-      const int r = lane / SLOTS, c = lane % SLOTS ^ R::swizzle(ROWS * i + r);
-      const int t = c * R::CHUNK < n ? c * R::CHUNK : 0;  // what is past the end is masked
-      dma16(uniform_ptr(at + (int64_t)(ROWS * i) * vt_ld),
-            (uint32_t)r * (uint32_t)(vt_ld * sizeof(T)) + (uint32_t)(t * sizeof(T)),
+    for (uint32_t i = 0; i < 16 / ROWS; ++i) {
+      const uint32_t t = c ^ R::swizzle(ROWS * i) * 16;
+      // what is past the end is masked
+      dma16(uniform_ptr(at + (int64_t)(ROWS * i) * vt_ld), row + (t < n * sizeof(T) ? t : 0),
             lds + i * 1024);
     }
   }
-  __device__ __forceinline__ void read(uint32_t lds, int lane) {
+  __device__ __forceinline__ void read(uint32_t lds, uint32_t lane) {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
       v[ks] = score_operand(lds + R::at(lane & 15, 8 * (lane >> 4)), 32 * ks, 0, T());
@@ -773,7 +775,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
   auto chunk = [&](auto whole_chunk, int n, bool update) {
     constexpr bool WHOLE = decltype(whole_chunk)::value;
     // made afresh in each chunk: what follows from it is more than registers hold
-    const int lane = (int)afresh(threadIdx.x & 63), col = lane & 15, g = lane >> 4;
+    const uint32_t lane = afresh(threadIdx.x & 63), col = lane & 15, g = lane >> 4;
     barrier_all();
     const bool more = c0 + kChunk < end;
     if (more) load_k(c0 + kChunk, next, lane);
@@ -781,7 +783,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     const uint32_t along = afresh(R::at(col, 4 * g));
 #pragma unroll(D == 64 ? 3 : 1)
     for (int i = 0; i < n_tiles; ++i) {
-      const int tq = tiles >> (4 * i + 2) & 3, st = tiles >> (4 * i) & 3;
+      const uint32_t tq = tiles >> (4 * i + 2) & 3, st = tiles >> (4 * i) & 3;
       f32x4 p = {0.f, 0.f, 0.f, 0.f};
       if (D == 64 || st <= tq) {
         const uint32_t k_tile = (along ^ R::tile_bits(st)) + buf + 16 * st * R::BYTES;
@@ -790,7 +792,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
         for (int kk = 0; kk < D / 32; ++kk)
           p = mma(split_operand<D>(k_tile, 32 * kk, 0, T()), split_operand<D>(q_tile, 32 * kk, 0, T()), p);
       }
-      const int far = 16 * (tq - st) + col - 4 * g;  // from the lane's first key
+      const int far = (int)(16 * (tq - st) + col - 4 * g);  // from the lane's first key
       if (D == 128 && st < tq) {
         const float w = a.scale * exp2_fast(-rate * (float)(far - 3));
 #pragma unroll
@@ -844,7 +846,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     T* at = o + c0 * o_ld + col * o_ld + 4 * g;
 #pragma unroll
     for (int tt = 0; tt < 4; ++tt) {
-      if (WHOLE || 16 * tt + col < n) store_out(at, out[tt]);
+      if (WHOLE || 16 * tt + (int)col < n) store_out(at, out[tt]);
       at += 16 * o_ld;
     }
     if (update) {
