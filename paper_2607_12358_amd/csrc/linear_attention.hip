@@ -762,13 +762,20 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
 #pragma unroll
   for (int tt = 0; tt < 4; ++tt) tile_decay[tt] = uniform(a.scale * exp2_fast(-rate * (float)(16 * tt)));
   // the scores' tiles of this wave, 4 tq + st a digit: tokens 16 tq .., keys 16
-  // st ..; the ten on and below the diagonal, and the two beside an even
-  // diagonal one, which come out as zeros
+  // st ..; the ten on and below the diagonal, the waves with one more than the
+  // others on different SIMDs (wave w's is w % 4).  The two beside an even diagonal
+  // tile are read too and stay zeros.
+  constexpr int TILES = D == 64 ? 2 : 1;
   const uint32_t tiles =
-      D == 64    ? (wave == 0 ? 0xf10 : wave == 1 ? 0xe54 : wave == 2 ? 0xa98 : 0xbdc)
-      : wave < 4 ? (wave == 0 ? 0x10 : wave == 1 ? 0x54 : wave == 2 ? 0x8 : 0x9)
-                 : (wave == 4 ? 0xba : wave == 5 ? 0xdc : wave == 6 ? 0xe : 0xf);
-  const int n_tiles = D == 64 ? 3 : wave < 2 || wave == 4 || wave == 5 ? 2 : 1;
+      D == 64    ? (wave == 0 ? 0xf0 : wave == 1 ? 0xe54 : wave == 2 ? 0xa98 : 0xdc)
+      : wave < 4 ? (wave == 0 ? 0x0 : wave == 1 ? 0x54 : wave == 2 ? 0x8 : 0x9)
+                 : (wave == 4 ? 0xa : wave == 5 ? 0xc : wave == 6 ? 0xed : 0xf);
+  const bool one_more = wave == 1 || wave == (D == 64 ? 2 : 6);
+  if (wave < 2) {
+    const int lane = threadIdx.x & 63, at = 32 * wave;
+    store_scores(scores + P::at(at + (lane & 15), at + 16 + 4 * (lane >> 4)), P::TOTAL,
+                 f32x4{0.f, 0.f, 0.f, 0.f}, T());
+  }
   __builtin_amdgcn_s_waitcnt(0);  // S is here: no wait for it among the chunks' loads
   int64_t c0 = begin;
   // One chunk of n tokens: 64, or (WHOLE false) a sequence's last ones.
@@ -781,29 +788,36 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     if (more) load_k(c0 + kChunk, next, lane);
     v.read(v_at, lane);
     const uint32_t along = afresh(R::at(col, 4 * g));
-#pragma unroll(D == 64 ? 3 : 1)
-    for (int i = 0; i < n_tiles; ++i) {
+    auto score_tile = [&](int i) {
       const uint32_t tq = tiles >> (4 * i + 2) & 3, st = tiles >> (4 * i) & 3;
-      f32x4 p = {0.f, 0.f, 0.f, 0.f};
-      if (D == 64 || st <= tq) {
-        const uint32_t k_tile = (along ^ R::tile_bits(st)) + buf + 16 * st * R::BYTES;
-        const uint32_t q_tile = (along ^ R::tile_bits(tq)) + q_at + 16 * tq * R::BYTES;
+      const uint32_t k_tile = (along ^ R::tile_bits(st)) + buf + 16 * st * R::BYTES;
+      const uint32_t q_tile = (along ^ R::tile_bits(tq)) + q_at + 16 * tq * R::BYTES;
+      Operand<T> kf[D / 32], qf[D / 32];
 #pragma unroll
-        for (int kk = 0; kk < D / 32; ++kk)
-          p = mma(split_operand<D>(k_tile, 32 * kk, 0, T()), split_operand<D>(q_tile, 32 * kk, 0, T()), p);
+      for (int kk = 0; kk < D / 32; ++kk) {
+        kf[kk] = split_operand<D>(k_tile, 32 * kk, 0, T());
+        qf[kk] = split_operand<D>(q_tile, 32 * kk, 0, T());
       }
       const int far = (int)(16 * (tq - st) + col - 4 * g);  // from the lane's first key
+      f32x4 w;
       if (D == 128 && st < tq) {
-        const float w = a.scale * exp2_fast(-rate * (float)(far - 3));
+        const float last = a.scale * exp2_fast(-rate * (float)(far - 3));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] *= w * pw.p[4 + i];
+        for (int i = 0; i < 4; ++i) w[i] = last * pw.p[4 + i];
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          p[i] = far >= i ? p[i] * (a.scale * exp2_fast(-rate * (float)(far - i))) : 0.f;
+        for (int i = 0; i < 4; ++i) w[i] = a.scale * exp2_fast(-rate * (float)(far - i));
       }
+      f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk) p = mma(kf[kk], qf[kk], p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = far >= i ? p[i] * w[i] : 0.f;
       store_scores(scores + P::at(16 * tq + col, 16 * st + 4 * g), P::TOTAL, p, T());
-    }
+    };
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) score_tile(i);
+    if (one_more) score_tile(TILES);
     if (more) {
       wait_lds();  // v is in its registers
       load_v(c0 + kChunk, lane);
@@ -896,15 +910,24 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_chunk_kernel
 // segment a head once the heads alone do).  With 256 / 512 workgroups: 12 x 4680
 // tokens (d = 128) 44 / 49 us, 1 x 30000 43 / 61, 4 x 8192 (d = 64) 24 / 30, but 12
 // x 32760 178 / 171.
+//
+// A bf16 chunk takes about as long as its segment's state costs to write, sum and
+// read, so segments have two unless there are few of them (one chunk / two,
+// d = 128: 32 x 512 tokens 33 / 24 us, 16 x 640 24 / 22, but 8 x 1024 23.3 / 24.6, and
+// with d = 64 4 x 1559 13.5 / 15.1), and up to four stay together (64 x 256: 25 in
+// four segments, 21 in two, 19 in one).  An fp32 chunk takes three times as long
+// (8 x 2000: one 44 us, two 54).
 struct Segments {
   int64_t tokens, count;
 };
-Segments segments_of(int64_t heads, int64_t L) {
+Segments segments_of(int dtype, int64_t heads, int64_t L) {
   const int64_t chunks = (L + kChunk - 1) / kChunk;
   const int64_t groups = heads * chunks >= 512 * 8 ? 512 : 256;
   const int64_t most = heads > 0 ? groups / heads : 1;
-  if (chunks <= 1 || most <= 1) return {chunks * kChunk, 1};
-  const int64_t per = (chunks + most - 1) / most;
+  const bool quick = dtype == ACID_BF16;
+  if (chunks <= (quick ? 4 : 1) || most <= 1) return {chunks * kChunk, 1};
+  int64_t per = (chunks + most - 1) / most;
+  if (quick && per == 1 && heads * chunks > 128) per = 2;
   return {per * kChunk, (chunks + per - 1) / per};
 }
 
@@ -953,7 +976,7 @@ size_t acid_linear_attention_workspace_bytes(int64_t n_seq, int32_t n_heads, int
       seq_len > kMaxTokens)
     return 0;
   const int64_t heads = n_seq * n_heads;
-  const Segments seg = segments_of(heads, seq_len);
+  const Segments seg = segments_of(ACID_F32, heads, seq_len);  // no fewer than in bf16
   return seg.count > 1 ? (size_t)(seg.count * heads * head_dim * head_dim * 4) : 0;
 }
 
@@ -994,7 +1017,7 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
   if (state_in_dev != state_out_dev &&
       bytes_overlap(state_in_dev, states, state_out_dev, states))
     return set_error(ACID_ERR_INVALID_ARG, "state_in and state_out: one buffer or apart");
-  const Segments seg = segments_of(heads, seq_len);
+  const Segments seg = segments_of(dtype, heads, seq_len);
   if (seg.count > 1) {
     const int64_t need = seg.count * states;
     if ((int64_t)workspace_bytes < need || !workspace_dev)

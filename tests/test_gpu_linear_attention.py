@@ -82,7 +82,8 @@ CASES = [  # n, heads, L, d, lengths
     (1, 1, 63, 64, None), (1, 2, 64, 128, None), (1, 2, 65, 64, None), (2, 2, 100, 128, [0, 100]),
     (3, 2, 129, 64, [129, 64, 65]), (2, 2, 200, 128, [-5, 1000]), (1, 3, 511, 64, None),
     (1, 2, 777, 128, None), (4, 1, 1100, 64, [1100, 1, 512, 1025]), (1, 2, 2500, 128, None),
-    (1, 1, 3001, 64, None), (2, 1, 4100, 128, [4100, 2049])]
+    (1, 1, 3001, 64, None), (2, 1, 4100, 128, [4100, 2049]), (1, 2, 256, 128, None),
+         (1, 2, 257, 64, None), (2, 8, 620, 64, [620, 301]), (4, 5, 640, 128, [640, 128, 129, 513])]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
