@@ -164,15 +164,18 @@ hipError_t launch_step(int dtype, int d, const StepArgs& a, hipStream_t s) {
 // K's operand of the outer products lies across those rows; bf16 reads it with
 // the transposing LDS load.
 //
-// 12 heads of 32760 tokens (d = 128, bf16) take 166 us in three launches: the
-// segments' states 51 us (232 MB), the scan of them 12 (62 MB) and the outputs 99
-// (431 MB), 4.3 to 5.2 TB/s where a copy makes 5.0; K and V are read twice,
-// because a segment's outputs need the states of those before it.  The outputs'
-// kernel keeps its vector units busy for half of that time too (S and the
-// scores made into operands, V decayed), with 16 waves a CU to hide it: 80 KB
-// of LDS and 128 registers a lane are what two workgroups have.  One wave for
-// 32 columns, half as many waves, took 115 us.  vt_ld = 32760 itself costs 10%:
-// rows that are no multiple of 128 bytes apart take two lines for one.
+// 12 heads of 32760 tokens (d = 128, bf16) take 162 us in three launches: the
+// segments' states 51 us (239 MB), the scan of them 12 (62 MB) and the outputs 95
+// (480 MB), 4.7 to 5.2 TB/s where a copy makes 5.0.  K and V are read twice,
+// because a segment's outputs need the states of those before it, and V's lines
+// that two chunks share come from beyond L2 again for the second now and then
+// (45 MB; the last reads of Q and K marked as such halve that, but 1 x 30000 with d
+// = 64 then takes 88 us for 85).  With all reads from L2 the outputs took 94 us for 97:
+// the vector units issue for half of that time (S and the scores made into
+// operands, V decayed), with 16 waves a CU to hide the rest: 80 KB of LDS and 128
+// registers a lane are what two workgroups have.  One wave for 32 columns, half as
+// many waves, took 115 us.  A workgroup alone on its CU takes 3.7 us a chunk (d =
+// 64: 2.3), mostly LDS loads, products and barriers waiting on one another.
 //
 // Rounding.  A bf16 operand made from fp32 values would cost the output half
 // of its accuracy, so scores and S go into their products as two bf16 parts
@@ -908,8 +911,8 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_chunk_kernel
 // Tokens of a segment, a multiple of 64, and how many there are: as many as
 // give each CU a workgroup, or two where they then have eight chunks each (one
 // segment a head once the heads alone do).  With 256 / 512 workgroups: 12 x 4680
-// tokens (d = 128) 44 / 49 us, 1 x 30000 43 / 61, 4 x 8192 (d = 64) 24 / 30, but 12
-// x 32760 178 / 171.
+// tokens (d = 128) 42 / 48 us, 1 x 30000 42 / 61, 4 x 8192 (d = 64) 23 / 29, but 12
+// x 32760 167 / 157 and 24 x 32760 318 / 301.
 //
 // A bf16 chunk takes about as long as its segment's state costs to write, sum and
 // read, so segments have two unless there are few of them (one chunk / two,
@@ -932,9 +935,10 @@ Segments segments_of(int dtype, int64_t heads, int64_t L) {
 }
 
 // Up to this many segments the outputs' kernel adds those before its own
-// itself; more take a scan, a launch of its own (4 segments, d = 128: 16.9 us
-// for 18.5; 13: 30.9 for 28.6; 25, d = 64: 21.7 for 18.9).
-constexpr int64_t kFolded = 8;
+// itself; more take a scan, a launch of its own (folded / scanned, d = 128: 6
+// segments of 24 x 1500 tokens 35.9 / 36.8 us, 8 of 32 x 2000 47.1 / 44.9; d = 64: 8 of
+// 32 x 2000 24.3 / 26.0, 25 of 4 x 1559 16.8 / 12.8).
+int64_t most_folded(int d) { return d == 64 ? 8 : 6; }
 
 template <typename T, int D>
 hipError_t launch_chunks(const ChunkArgs& a, int64_t heads, hipStream_t s) {
@@ -1036,7 +1040,7 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
   const ChunkArgs a = {q_dev, k_dev, vt_dev, o_dev, vt_ld, slopes_dev, lengths_dev, state_in_dev,
                        state_out_dev, seg.count > 1 ? (float*)workspace_dev : nullptr, seq_len,
                        n_heads, (int32_t)seg.count, (int32_t)seg.tokens,
-                       seg.count > kFolded, scale};
+                       seg.count > most_folded(head_dim), scale};
   hipError_t e;
   if (dtype == ACID_BF16)
     e = head_dim == 64 ? launch_chunks<bf16, 64>(a, heads, stream)
