@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 from typing import Iterable, Optional, Sequence
 
 import numpy as np
@@ -185,28 +186,29 @@ def _dtype_code(torch, t, name: str) -> int:
     raise ValueError(f"{name}: expected bfloat16 or float32, got {t.dtype}")
 
 
-def _device(t, name: str):
-    if not t.is_cuda:
+def _device(t, name: str) -> int:
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError(f"{name}: expected a tensor on a GPU, got one on {t.device}")
-    return t.device
+    return dev
 
 
 def _at(dev, name: str, t, shape: tuple, dtype) -> Optional[int]:
-    """Address of t (or None): a contiguous tensor on dev of this shape and type."""
+    """Address of t (or None): a contiguous tensor on GPU dev of this shape and type."""
     if t is None:
         return None
-    if t.shape == shape and t.dtype is dtype and t.device == dev and t.is_contiguous():
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
         return t.data_ptr()
-    if t.device != dev:
-        raise ValueError(f"{name}: expected a tensor on {dev}, got {t.device}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: expected a tensor on GPU {dev}, got one on {t.device}")
     raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {shape}, "
                      f"got {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
 
 
 def _rows_at(dev, name: str, t, shape: tuple, dtype):
-    """(address, row stride) of a matrix on dev of this shape and type, of unit
+    """(address, row stride) of a matrix on GPU dev of this shape and type, of unit
     column stride; of one row the stride counts as whole 16 bytes."""
-    if t.shape == shape and t.dtype is dtype and t.device == dev:
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev:
         rows, cols = shape
         ld, unit = t.stride()
         if unit == 1 or cols == 1:
@@ -215,21 +217,21 @@ def _rows_at(dev, name: str, t, shape: tuple, dtype):
             if ld >= cols:
                 return t.data_ptr(), ld
         raise ValueError(f"{name}: expected unit column stride and rows apart, got strides {t.stride()}")
-    if t.device != dev:
-        raise ValueError(f"{name}: expected a tensor on {dev}, got {t.device}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: expected a tensor on GPU {dev}, got one on {t.device}")
     raise ValueError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)}")
 
 
 def _on(torch, dev, stream, fn, *args) -> None:
-    """fn(*args, stream) on `dev`: the stream given, which has to be that
+    """fn(*args, stream) on GPU `dev`: the stream given, which has to be that
     device's, or its current one."""
     if stream is not None:
-        if stream.device != dev:
-            raise ValueError(f"stream of {stream.device} for tensors on {dev}")
+        if stream.device.index != dev:
+            raise ValueError(f"stream of {stream.device} for tensors on GPU {dev}")
         raw = stream.cuda_stream
     else:
-        raw = torch._C._cuda_getCurrentRawStream(dev.index)
-    if dev.index != torch.cuda.current_device():
+        raw = torch._C._cuda_getCurrentRawStream(dev)
+    if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):  # what the null stream means
             status = fn(*args, raw)
     else:
@@ -306,6 +308,8 @@ def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
         d ** -0.5 if scale is None else scale, *_rows_at(dev, "o", o, shape, dt))
 
 
+# acid_residual_norm_args, packed in a quarter of the time its ctypes form takes
+_NORM_ARGS = struct.Struct("@PqPqPqPqiiiiPPPPPqff")
 _NORMS = {"none": ACID_NORM_NONE, "layer": ACID_NORM_LAYER, "rms": ACID_NORM_RMS}
 
 
@@ -331,20 +335,20 @@ def residual_norm(h, y=None, h_out=None, out=None, res_scale: float = 1.0, post:
     dev, shape = _device(h, "h"), tuple(h.shape)
     rows, hidden = shape
     n_mod = -(-rows // rows_per_mod) if rows_per_mod else 1
-    nothing = (None, 0)
+    nothing = (0, 0)
 
     def vector(name, t):
         one = t is not None and n_mod == 1 and t.dim() == 1
-        return _at(dev, name, t, (hidden,) if one else (n_mod, hidden), f32)
+        return _at(dev, name, t, (hidden,) if one else (n_mod, hidden), f32) or 0
 
     h_at = _rows_at(dev, "h", h, shape, f32)
-    a = _L.ResidualNormArgsC(
+    a = _NORM_ARGS.pack(
         *h_at, *(nothing if y is None else _rows_at(dev, "y", y, shape, y.dtype)),
         *(h_at if h_out is None else _rows_at(dev, "h_out", h_out, shape, f32)),
         *(nothing if out is None else _rows_at(dev, "out", out, shape, out.dtype)),
         0 if y is None else _dtype_code(torch, y, "y"), 0 if out is None else _dtype_code(torch, out, "out"),
-        _NORMS[post], _NORMS[pre], _at(dev, "post_weight", post_weight, (hidden,), f32),
-        _at(dev, "pre_weight", pre_weight, (hidden,), f32), vector("gate", gate),
+        _NORMS[post], _NORMS[pre], _at(dev, "post_weight", post_weight, (hidden,), f32) or 0,
+        _at(dev, "pre_weight", pre_weight, (hidden,), f32) or 0, vector("gate", gate),
         vector("shift", shift), vector("scale", scale), rows_per_mod, res_scale, eps)
     _on(torch, dev, stream, lib().acid_residual_norm, a, rows, hidden)
 
@@ -361,12 +365,11 @@ def w4_shapes(n: int, k: int, group: int = 128):
 def _w4_at(torch, x, codes, scales, n: int, k: int):
     """(x's device, group, codes' address, scales' address)."""
     groups = scales.shape[1] if scales.dim() == 3 else 0
-    if groups < 1 or k % groups or codes.dim() != 4:
+    if groups < 1 or k % groups or k % 128 or codes.dim() != 4:
         raise ValueError("codes, scales: see w4_shapes")
-    group = k // groups
-    cs, ss = w4_shapes(n, k, group)
-    dev = _device(x, "x")
-    return dev, group, _at(dev, "codes", codes, cs, torch.uint8), _at(dev, "scales", scales, ss, torch.float32)
+    tiles, dev = -(-n // 16), _device(x, "x")
+    return (dev, k // groups, _at(dev, "codes", codes, (tiles, k // 128, 64, 16), torch.uint8),
+            _at(dev, "scales", scales, (tiles, groups, 16), torch.float32))
 
 
 def quantize_w4(w, codes, scales, stream=None) -> None:

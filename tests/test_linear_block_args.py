@@ -94,6 +94,11 @@ def _norm(lib, rows=10, hidden=256, **kw):
     return lib.acid_residual_norm(C.byref(a), rows, hidden, None)
 
 
+def test_packed_norm_arguments_are_the_structs_bytes():
+    values = [*range(1, 19), 0.5, 0.25]
+    assert P._NORM_ARGS.pack(*values) == bytes(L.ResidualNormArgsC(*values))
+
+
 @pytest.mark.parametrize("kw,status", [
     (dict(rows=-1), BAD), (dict(hidden=0), SHAPE), (dict(hidden=258), SHAPE),
     (dict(hidden=8196), SHAPE), (dict(rows=(1 << 23) + 1), SHAPE), (dict(post=3), BAD),
