@@ -173,8 +173,9 @@ def linear(a, wt, kind: int, bias, gate=None, out=None, v_out=None, q=None, k=No
 
 # ------------------------------------------------ linear-attention block
 #
-# A call for a few tokens is bound by the host, so what these functions do per
-# tensor is kept short: one test that holds, its parts only where it does not.
+# A call for a few tokens is bound by the host, so tensors are looked at by the
+# native module _binding, which calls _at and _rows_at below for those that are
+# not as they have to be, and calls the library.
 
 
 def _dtype_code(torch, t, name: str) -> int:
@@ -222,6 +223,26 @@ def _rows_at(dev, name: str, t, shape: tuple, dtype):
     raise ValueError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)}")
 
 
+_bound = None
+
+
+def _native():
+    """torch, and the native module, bound to it and to the library."""
+    global _bound
+    if _bound is None:
+        torch = _torch()
+        try:
+            from . import _binding as N
+        except ImportError as e:
+            raise RuntimeError("_binding.so is missing: build it with "
+                               "`python -m paper_2607_12358_amd.build`") from e
+        N.bind(getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), torch.Tensor, _at, _rows_at,
+               ((torch.bfloat16, 4, 16), (torch.float32, 2, 32), (torch.int32, 0, 32), (torch.uint8, 1, 8)),
+               {name: C.cast(getattr(lib(), name), C.c_void_p).value for name in _L._SIGS})
+        _bound = torch, N, N.at, N.rows_at
+    return _bound
+
+
 def _on(torch, dev, stream, fn, *args) -> None:
     """fn(*args, stream) on GPU `dev`: the stream given, which has to be that
     device's, or its current one."""
@@ -256,7 +277,7 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
     left as they are.  workspace: uint8 tensor of linear_attention_workspace
     bytes, kept by callers whose calls must not allocate; by default one is
     taken from torch's allocator for the call."""
-    torch = _torch()
+    torch, N, at, rows_at = _native()
     if q.dim() not in (3, 4):
         raise ValueError("q: expected [heads, L, d] or [n_seq, heads, L, d]")
     code, dev, lead, dt = _dtype_code(torch, q, "q"), _device(q, "q"), tuple(q.shape[:-3]), q.dtype
@@ -265,14 +286,14 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
     if vt.dim() != q.dim():
         raise ValueError("vt: expected as many axes as q")
     states, vt_ld = lead + (n_heads, d, d), vt.shape[-1]
-    args = (_at(dev, "q", q, lead + (n_heads, L, d), dt), _at(dev, "k", k, lead + (n_heads, L, d), dt),
-            _at(dev, "vt", vt, lead + (n_heads, d, vt_ld), dt), vt_ld,
-            _at(dev, "slopes", slopes, (n_heads,), torch.float32),
-            _at(dev, "lengths", lengths, (n_seq,), torch.int32),
-            _at(dev, "state_in", state_in, states, torch.float32),
-            _at(dev, "state_out", state_out, states, torch.float32),
+    args = (at(dev, "q", q, lead + (n_heads, L, d), dt), at(dev, "k", k, lead + (n_heads, L, d), dt),
+            at(dev, "vt", vt, lead + (n_heads, d, vt_ld), dt), vt_ld,
+            at(dev, "slopes", slopes, (n_heads,), torch.float32),
+            at(dev, "lengths", lengths, (n_seq,), torch.int32),
+            at(dev, "state_in", state_in, states, torch.float32),
+            at(dev, "state_out", state_out, states, torch.float32),
             d ** -0.5 if scale is None else scale,
-            _at(dev, "o", o, lead + (L, n_heads * d), dt))
+            at(dev, "o", o, lead + (L, n_heads * d), dt))
     if workspace is None:
         size = lib().acid_linear_attention_workspace_bytes(n_seq, n_heads, L, d)
         if size:
@@ -280,8 +301,8 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
                 workspace = torch.empty(size, dtype=torch.uint8, device=dev)
     else:
         size = workspace.numel()
-    _on(torch, dev, stream, lib().acid_linear_attention, code, n_seq, n_heads, L, d, *args,
-        None if workspace is None else _at(dev, "workspace", workspace, (size,), torch.uint8), size)
+    _on(torch, dev, stream, N.linear_attention, code, n_seq, n_heads, L, d, *args,
+        None if workspace is None else at(dev, "workspace", workspace, (size,), torch.uint8), size)
 
 
 def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
@@ -292,20 +313,20 @@ def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
     given; slots int32 [rows]: each row's state (default: its own index), any
     value outside [0, n_slots) marking a padding row that is left alone; rows
     of one slot are successive tokens, in row order (at most 65536 rows)."""
-    torch = _torch()
+    torch, N, at, rows_at = _native()
     if state.dim() != 4:
         raise ValueError("state: expected [n_slots, heads, d, d]")
     code, dev, dt = _dtype_code(torch, q, "q"), _device(state, "state"), q.dtype
     n_slots, n_heads, d = state.shape[:3]
     rows, states = q.shape[0], (n_slots, n_heads, d, d)
     shape = (rows, n_heads * d)
-    at = _at(dev, "state", state, states, torch.float32)
-    _on(torch, dev, stream, lib().acid_linear_attention_step, code, rows, n_heads, d,
-        *_rows_at(dev, "q", q, shape, dt), *_rows_at(dev, "k", k, shape, dt),
-        *_rows_at(dev, "v", v, shape, dt), _at(dev, "slopes", slopes, (n_heads,), torch.float32),
-        _at(dev, "slots", slots, (rows,), torch.int32), n_slots, at,
-        at if state_out is None else _at(dev, "state_out", state_out, states, torch.float32),
-        d ** -0.5 if scale is None else scale, *_rows_at(dev, "o", o, shape, dt))
+    state_at = at(dev, "state", state, states, torch.float32)
+    _on(torch, dev, stream, N.linear_attention_step, code, rows, n_heads, d,
+        *rows_at(dev, "q", q, shape, dt), *rows_at(dev, "k", k, shape, dt),
+        *rows_at(dev, "v", v, shape, dt), at(dev, "slopes", slopes, (n_heads,), torch.float32),
+        at(dev, "slots", slots, (rows,), torch.int32), n_slots, state_at,
+        state_at if state_out is None else at(dev, "state_out", state_out, states, torch.float32),
+        d ** -0.5 if scale is None else scale, *rows_at(dev, "o", o, shape, dt))
 
 
 # acid_residual_norm_args, packed in a quarter of the time its ctypes form takes
@@ -322,7 +343,7 @@ def residual_norm(h, y=None, h_out=None, out=None, res_scale: float = 1.0, post:
     or fp32, either may be None; norms "none", "layer" or "rms"; weights fp32
     [hidden]; gate, shift, scale fp32 [hidden], or [n_mod, hidden] with row r
     using row r // rows_per_mod.  Matrices may be row-strided."""
-    torch = _torch()
+    torch, N, at, rows_at = _native()
     f32 = torch.float32
     if post not in _NORMS or pre not in _NORMS:
         raise ValueError(f"unknown norm {post if post not in _NORMS else pre!r}")
@@ -339,18 +360,18 @@ def residual_norm(h, y=None, h_out=None, out=None, res_scale: float = 1.0, post:
 
     def vector(name, t):
         one = t is not None and n_mod == 1 and t.dim() == 1
-        return _at(dev, name, t, (hidden,) if one else (n_mod, hidden), f32) or 0
+        return at(dev, name, t, (hidden,) if one else (n_mod, hidden), f32) or 0
 
-    h_at = _rows_at(dev, "h", h, shape, f32)
+    h_at = rows_at(dev, "h", h, shape, f32)
     a = _NORM_ARGS.pack(
-        *h_at, *(nothing if y is None else _rows_at(dev, "y", y, shape, y.dtype)),
-        *(h_at if h_out is None else _rows_at(dev, "h_out", h_out, shape, f32)),
-        *(nothing if out is None else _rows_at(dev, "out", out, shape, out.dtype)),
+        *h_at, *(nothing if y is None else rows_at(dev, "y", y, shape, y.dtype)),
+        *(h_at if h_out is None else rows_at(dev, "h_out", h_out, shape, f32)),
+        *(nothing if out is None else rows_at(dev, "out", out, shape, out.dtype)),
         0 if y is None else _dtype_code(torch, y, "y"), 0 if out is None else _dtype_code(torch, out, "out"),
-        _NORMS[post], _NORMS[pre], _at(dev, "post_weight", post_weight, (hidden,), f32) or 0,
-        _at(dev, "pre_weight", pre_weight, (hidden,), f32) or 0, vector("gate", gate),
+        _NORMS[post], _NORMS[pre], at(dev, "post_weight", post_weight, (hidden,), f32) or 0,
+        at(dev, "pre_weight", pre_weight, (hidden,), f32) or 0, vector("gate", gate),
         vector("shift", shift), vector("scale", scale), rows_per_mod, res_scale, eps)
-    _on(torch, dev, stream, lib().acid_residual_norm, a, rows, hidden)
+    _on(torch, dev, stream, N.residual_norm, a, rows, hidden)
 
 
 def w4_shapes(n: int, k: int, group: int = 128):
@@ -362,24 +383,24 @@ def w4_shapes(n: int, k: int, group: int = 128):
     return (tiles, k // 128, 64, 16), (tiles, k // group, 16)
 
 
-def _w4_at(torch, x, codes, scales, n: int, k: int):
+def _w4_at(torch, at, x, codes, scales, n: int, k: int):
     """(x's device, group, codes' address, scales' address)."""
     groups = scales.shape[1] if scales.dim() == 3 else 0
     if groups < 1 or k % groups or k % 128 or codes.dim() != 4:
         raise ValueError("codes, scales: see w4_shapes")
     tiles, dev = -(-n // 16), _device(x, "x")
-    return (dev, k // groups, _at(dev, "codes", codes, (tiles, k // 128, 64, 16), torch.uint8),
-            _at(dev, "scales", scales, (tiles, groups, 16), torch.float32))
+    return (dev, k // groups, at(dev, "codes", codes, (tiles, k // 128, 64, 16), torch.uint8),
+            at(dev, "scales", scales, (tiles, groups, 16), torch.float32))
 
 
 def quantize_w4(w, codes, scales, stream=None) -> None:
     """codes, scales (w4_shapes) of the fp32 weight w [k inputs, n outputs]."""
-    torch = _torch()
+    torch, N, at, rows_at = _native()
     if w.dim() != 2:
         raise ValueError("w: expected [k, n]")
     k, n = w.shape
-    dev, group, c, s = _w4_at(torch, w, codes, scales, n, k)
-    _on(torch, dev, stream, lib().acid_quantize_w4, _at(dev, "w", w, (k, n), torch.float32), n, k, group,
+    dev, group, c, s = _w4_at(torch, at, w, codes, scales, n, k)
+    _on(torch, dev, stream, N.quantize_w4, at(dev, "w", w, (k, n), torch.float32), n, k, group,
         c, s)
 
 
@@ -387,16 +408,16 @@ def linear_w4(x, codes, scales, out, bias=None, gelu: bool = False, stream=None)
     """out = act(x w^T + bias) for few rows x [m, k] (bf16 or fp32) and 4-bit
     weights (quantize_w4); out [m, n] bf16 or fp32; bias fp32 [n].  x and out
     may be row-strided."""
-    torch = _torch()
+    torch, N, at, rows_at = _native()
     if x.dim() != 2 or out.dim() != 2:
         raise ValueError("x and out: expected two axes")
     (m, k), n = x.shape, out.shape[1]
-    dev, group, c, s = _w4_at(torch, x, codes, scales, n, k)
-    _on(torch, dev, stream, lib().acid_linear_w4, _dtype_code(torch, x, "x"), m, n, k, group,
-        *_rows_at(dev, "x", x, (m, k), x.dtype), c, s,
-        _at(dev, "bias", bias, (n,), torch.float32),
+    dev, group, c, s = _w4_at(torch, at, x, codes, scales, n, k)
+    _on(torch, dev, stream, N.linear_w4, _dtype_code(torch, x, "x"), m, n, k, group,
+        *rows_at(dev, "x", x, (m, k), x.dtype), c, s,
+        at(dev, "bias", bias, (n,), torch.float32),
         ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS, _dtype_code(torch, out, "out"),
-        *_rows_at(dev, "out", out, (m, n), out.dtype))
+        *rows_at(dev, "out", out, (m, n), out.dtype))
 
 
 # ------------------------------------------------------------------ model

@@ -125,7 +125,7 @@ _SIGS = {
     "acid_linear_attention_step": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, C.c_int32,
                                              _P, C.c_int64, _P, C.c_int64, _P, C.c_int64, _P, _P,
                                              C.c_int64, _P, _P, C.c_float, _P, C.c_int64, _P]),
-    "acid_residual_norm": (C.c_int, [_P, C.c_int64, C.c_int32, _P]),  # ResidualNormArgsC, or its bytes
+    "acid_residual_norm": (C.c_int, [C.POINTER(ResidualNormArgsC), C.c_int64, C.c_int32, _P]),
     "acid_quantize_w4": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]),
     "acid_linear_w4": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, _P,
                                  C.c_int64, _P, _P, _P, C.c_int32, C.c_int32, _P, C.c_int64, _P]),

@@ -4,7 +4,8 @@
 
 Every HIP source is compiled for gfx950 with packed-fp32 instructions
 disabled; the gate is host code compiled without floating-point contraction.
-Objects go to ``_build/``; the shared library lands next to this file.
+What the binding does natively is a Python module of its own, _binding.so.
+Objects go to ``_build/``; the shared libraries land next to this file.
 """
 from __future__ import annotations
 
@@ -13,6 +14,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -20,6 +22,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libacid.so")
+BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
 HIP_SOURCES = ["elementwise.hip", "temb.hip", "gemm.hip", "attention.hip", "runtime.hip",
@@ -54,17 +57,23 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _link(target: str, *args: str) -> None:
+    tmp = target + ".tmp"
+    cmd = [hipcc(), "-shared", "-fPIC", *args, "-o", tmp]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, target)
+
+
 def build(verbose: bool = True) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = HIP_SOURCES + HOST_SOURCES
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         objs = list(ex.map(_compile, srcs))
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, LIB)
+    _link(LIB, f"--offload-arch={ARCH}", *objs)
+    _link(BINDING, *_flags_common(), f"-I{sysconfig.get_paths()['include']}",
+          os.path.join(CSRC, "binding.cpp"))
     if verbose:
         print(f"built {LIB}")
     return LIB

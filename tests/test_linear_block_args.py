@@ -178,3 +178,44 @@ def test_binding_refuses_wrong_tensors():
     with pytest.raises(ValueError, match="w4_shapes"):
         P.linear_w4(t(1, 128), t(1, 64), t(1, 1, 16), t(1, 16))
     assert P.w4_shapes(17, 256, 32) == ((2, 2, 64, 16), (2, 8, 16))
+
+
+class _Native:
+    """The entry points as the binding calls them."""
+
+    def __getattr__(self, name):
+        return getattr(P._native()[1], name.removeprefix("acid_"))
+
+
+def test_native_calls_pass_every_argument_on(lib):
+    """A refusal for each argument in turn, in the same words by both ways."""
+    def both(call, **kw):
+        statuses = []
+        for how in (lib, _Native()):
+            statuses.append((call(how, **kw), L.last_error()))
+        assert statuses[0] == statuses[1] and statuses[0][0] != 0, kw
+
+    for kw in (dict(dtype=7), dict(n=-1), dict(heads=1 << 21), dict(L=-1), dict(d=80), dict(q=None), dict(k=3 * G),
+               dict(k=None), dict(vt=G + 8), dict(ld=99), dict(ld=1 << 40), dict(slopes=None), dict(sin=5 * G),
+               dict(sout=G), dict(o=None), dict(L=40000, ld=40000, ws=None), dict(L=40000, ld=40000, bytes=77)):
+        if "bytes" in kw or "ws" in kw:
+            kw.update(n=1, heads=2, d=128)
+        both(_attend, **kw)
+    for kw in (dict(dtype=2), dict(rows=-1), dict(rows=65537), dict(heads=0), dict(d=32), dict(q=None), dict(qld=120),
+               dict(k=G + 2), dict(kld=385), dict(v=None), dict(vld=1 << 33), dict(slopes=None), dict(slots=None, n_slots=3),
+               dict(n_slots=-1), dict(sin=None), dict(sout=4 * G + 8), dict(o=4 * G), dict(old=64)):
+        both(_step, **kw)
+    for kw in (dict(M=-1), dict(N=0), dict(K=200), dict(group=16), dict(x=None), dict(codes=2 * G + 8), dict(scales=None),
+               dict(out=None)):
+        both(_w4, **kw)
+    native = _Native()
+    a = L.ResidualNormArgsC()
+    for args in ((bytes(a), -1, 256, None), (bytes(a), 4, 6, None), (None, 4, 256, None), (bytes(a), 4, 256, None)):
+        assert native.acid_residual_norm(*args) == BAD or args[2] == 6
+    assert native.acid_quantize_w4(G, 100, 256, 48, 2 * G, 3 * G, None) == SHAPE
+    with pytest.raises(TypeError):
+        native.acid_quantize_w4(G, 100, 256)
+    with pytest.raises(OverflowError):
+        native.acid_quantize_w4(G, 1 << 31, 256, 64, 2 * G, 3 * G, None)
+    with pytest.raises(TypeError):
+        native.acid_quantize_w4(G, 100.0, 256, 64, 2 * G, 3 * G, None)
