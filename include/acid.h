@@ -471,11 +471,16 @@ acid_status acid_block_forward(acid_model* m, int32_t block,
  * Products are accumulated, and states kept, in fp32.  q, k, v and the state
  * must be finite: a NaN or an infinity spoils its head's outputs from 63
  * tokens before it on.
- * Workspace: acid_linear_attention_workspace_bytes(...) bytes (0: may be
+ * Workspace: acid_linear_attention_workspace_needed(...) bytes (0: may be
  * NULL), 16-byte aligned, not shared by calls that may overlap; ACID_ERR_SHAPE
- * if it is smaller.  Buffers 16-byte aligned, outputs apart from inputs. */
+ * if it is smaller.  in_place: state_out is state_in; a state apart lets shorter
+ * sequences do without workspace, in one launch.  ..._bytes(...) is enough for
+ * both types, in place too.  Buffers 16-byte aligned, outputs apart from inputs. */
 size_t acid_linear_attention_workspace_bytes(int64_t n_seq, int32_t n_heads,
                                              int64_t seq_len, int32_t head_dim);
+size_t acid_linear_attention_workspace_needed(int32_t dtype, int64_t n_seq, int32_t n_heads,
+                                              int64_t seq_len, int32_t head_dim,
+                                              int32_t in_place);
 acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
                                   int64_t seq_len, int32_t head_dim,
                                   const void* q_dev, const void* k_dev,

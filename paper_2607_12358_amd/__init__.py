@@ -262,7 +262,7 @@ def _on(torch, dev, stream, fn, *args) -> None:
 
 
 def linear_attention_workspace(n_seq: int, n_heads: int, seq_len: int, head_dim: int) -> int:
-    """Bytes of workspace linear_attention needs for these sizes."""
+    """Bytes of workspace that are enough for linear_attention of these sizes."""
     return int(lib().acid_linear_attention_workspace_bytes(n_seq, n_heads, seq_len, head_dim))
 
 
@@ -272,7 +272,8 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
     scale q_t S_t (scale defaults to 1/sqrt(d)).  q, k [n_seq, heads, L, d];
     vt [n_seq, heads, d, vt_ld]; o [n_seq, L, heads*d]; all bf16 or all fp32
     (attention's layouts; without the n_seq axis for one sequence).  slopes
-    fp32 [heads]; states fp32 [n_seq, heads, d, d], state_out may be state_in;
+    fp32 [heads]; states fp32 [n_seq, heads, d, d], state_out may be state_in
+    (apart, shorter sequences take one launch and no workspace);
     lengths int32 [n_seq]: tokens of each sequence, its later rows of o are
     left as they are.  workspace: uint8 tensor of linear_attention_workspace
     bytes, kept by callers whose calls must not allocate; by default one is
@@ -295,7 +296,8 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
             d ** -0.5 if scale is None else scale,
             at(dev, "o", o, lead + (L, n_heads * d), dt))
     if workspace is None:
-        size = lib().acid_linear_attention_workspace_bytes(n_seq, n_heads, L, d)
+        in_place = args[6] is not None and args[6] == args[7]
+        size = N.linear_attention_workspace_needed(code, n_seq, n_heads, L, d, in_place)
         if size:
             with torch.cuda.stream(stream):  # its memory goes back to that stream's pool
                 workspace = torch.empty(size, dtype=torch.uint8, device=dev)

@@ -119,6 +119,8 @@ _SIGS = {
                               C.POINTER(EpilogueArgsC), _P]),
     "acid_linear_attention_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int64,
                                                            C.c_int32]),
+    "acid_linear_attention_workspace_needed": (C.c_size_t, [C.c_int32, C.c_int64, C.c_int32,
+                                                            C.c_int64, C.c_int32, C.c_int32]),
     "acid_linear_attention": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_int32,
                                         _P, _P, _P, C.c_int64, _P, _P, _P, _P, C.c_float, _P, _P,
                                         C.c_size_t, _P]),

@@ -140,19 +140,18 @@ T value(PyObject* o) {
   }
 }
 
-template <typename... A, size_t... I>
-PyObject* convert_and_call(acid_status (*f)(A...), PyObject* const* args,
-                           std::index_sequence<I...>) {
+template <typename R, typename... A, size_t... I>
+PyObject* convert_and_call(R (*f)(A...), PyObject* const* args, std::index_sequence<I...>) {
   const std::tuple<A...> v{value<A>(args[I])...};
   if (PyErr_Occurred()) return nullptr;
-  acid_status status;
+  R result;
   Py_BEGIN_ALLOW_THREADS;
-  status = std::apply(f, v);
+  result = std::apply(f, v);
   Py_END_ALLOW_THREADS;
-  return PyLong_FromLong(status);
+  return PyLong_FromLongLong((long long)result);
 }
-template <typename... A>
-PyObject* call(acid_status (*f)(A...), PyObject* const* args, Py_ssize_t n) {
+template <typename R, typename... A>
+PyObject* call(R (*f)(A...), PyObject* const* args, Py_ssize_t n) {
   if (!f || n != (Py_ssize_t)sizeof...(A)) {
     PyErr_Format(PyExc_TypeError, f ? "%zd arguments, not %zd" : "bind() comes first",
                  (Py_ssize_t)sizeof...(A), n);
@@ -163,7 +162,8 @@ PyObject* call(acid_status (*f)(A...), PyObject* const* args, Py_ssize_t n) {
 
 // The library that ctypes has loaded gives the addresses.
 #define ENTRIES(E) \
-  E(linear_attention) E(linear_attention_step) E(residual_norm) E(linear_w4) E(quantize_w4)
+  E(linear_attention_workspace_needed) E(linear_attention) E(linear_attention_step)               \
+  E(residual_norm) E(linear_w4) E(quantize_w4)
 #define ENTRY(name)                                                       \
   decltype(&acid_##name) name##_address = nullptr;                        \
   PyObject* name(PyObject*, PyObject* const* args, Py_ssize_t n) {        \

@@ -6,6 +6,8 @@
 // S is fp32 [d][d] (rows over k's columns, columns over v's).  Both forms move
 // little more than they must: a token costs 4 d^2 operations a head for 4 d
 // values, a single token reads and writes its states.
+#include <math.h>
+
 #include <type_traits>
 
 #include "common.h"
@@ -184,6 +186,7 @@ hipError_t launch_step(int dtype, int d, const StepArgs& a, hipStream_t s) {
 // carried to another segment, V goes in as three parts, which is exact.
 constexpr int kChunk = 64;
 constexpr int64_t kMaxTokens = (int64_t)1 << 28;
+constexpr int kMaxAlone = 5;  // segments that make their own states
 
 template <typename T>
 struct Operand;  // eight values of the contracted index
@@ -520,10 +523,11 @@ struct ChunkArgs {
   const int32_t* lengths;
   const float* state_in;
   float* state_out;
-  float* slots;  // [n_seq][heads][segments][D][D], or null: one segment
+  float* slots;  // [n_seq][heads][segments][D][D], or null: each segment makes its own state
   int64_t tokens;
   int32_t heads, segments, segment;  // segment: tokens of one, a multiple of 64
   int32_t scanned;
+  int32_t cut[kMaxAlone - 1];  // slots null: where segments 1 .. begin
   float scale;
 };
 
@@ -731,7 +735,8 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     load_rows<T, D>(uniform_ptr(q + c0 * D), tokens(c0), q_at, wave, lane);
   };
   auto load_v = [&](int64_t c0, int lane) { V::load(vt + c0, a.vt_ld, tokens(c0), v_at, lane); };
-  if (begin < end) {
+  const bool alone = seg > 0 && !a.slots;  // makes its own state
+  if (begin < end && !alone) {
     const int lane = threadIdx.x & 63;
     load_k(begin, buf, lane);
     load_q(begin, lane);
@@ -739,7 +744,44 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
   }
 
   State<D> s;
-  if (seg == 0) {
+  if (alone) {
+    // As la_state_kernel does, from the sequence's start; the last step brings
+    // the first chunk's K and V.  V's second place is where Q's rows will be, of
+    // which each wave loads the bytes that were its V's.
+    const int lane = threadIdx.x & 63;
+    constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
+    static_assert((int)sizeof(T) * 1024 == V::BYTES, "Q's rows of a wave, V's place");
+    uint32_t v_now = q_at + wave * V::BYTES, v_next = v_at;
+    if (begin / kChunk % 2 == 0) {
+      v_now = v_at;
+      v_next = q_at + wave * V::BYTES;
+    }
+    load_k(0, buf, lane);
+    V::load(vt, a.vt_ld, kChunk, v_now, lane);
+    if (a.state_in) {
+      read_state(s, a.state_in + hs * (D * D));
+      const float w = (float)exp(-(double)slope * begin);
+      for_state(s, [&](f32x4& t, int, int, int) { t *= w; });
+    } else {
+      for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{0.f, 0.f, 0.f, 0.f}; });
+    }
+    for (int64_t c0 = 0; c0 < begin; c0 += kChunk) {
+      barrier_all();
+      load_k(c0 + kChunk, next, lane);
+      V::load(vt + c0 + kChunk, a.vt_ld, tokens(c0 + kChunk), v_next, lane);
+      v.read(v_now, lane);
+      add_outer<T, D, PARTS, true>(s, afresh(buf + column_base<T, D>(lane)), v, rate, pw,
+                                   (int)(begin - 1 - c0), lane);
+      uint32_t t = buf;
+      buf = next;
+      next = t;
+      t = v_now;
+      v_now = v_next;
+      v_next = t;
+    }
+    wait_lds();
+    load_q(begin, lane);
+  } else if (seg == 0) {
     if (!a.state_in)
       for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{0.f, 0.f, 0.f, 0.f}; });
     else if (a.slots && len > 0)
@@ -901,7 +943,11 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_chunk_kernel
   const int seg = blockIdx.x % a.segments;
   const int64_t hs = blockIdx.x / a.segments;
   const int64_t len = length_of(a.lengths, hs / a.heads, a.tokens);
-  const int64_t begin = (int64_t)seg * a.segment, end = begin + a.segment;
+  int64_t begin = (int64_t)seg * a.segment, end = begin + a.segment;
+  if (!a.slots) {
+    begin = seg > 0 ? a.cut[seg - 1] : 0;
+    end = seg + 1 < a.segments ? a.cut[seg] : a.tokens;
+  }
   if (end < len)
     chunks_of<T, D, false>(a, rows, seg, hs, len, begin, end);
   else if (seg == 0 || begin < len)
@@ -940,9 +986,58 @@ Segments segments_of(int dtype, int64_t heads, int64_t L) {
 // 32 x 2000 24.3 / 26.0, 25 of 4 x 1559 16.8 / 12.8).
 int64_t most_folded(int d) { return d == 64 ? 8 : 6; }
 
+// Segments that each make the state before them from the sequence's start: one
+// launch and no workspace, but the last of n segments goes through K and V of
+// all tokens (at r of the time that their outputs would take; cut for 0.3 to 0.5
+// the times are within 5%, best for 0.3 with d = 64 and for 0.4 with 128).
+constexpr double kStateShare = 0.4;
+double alone_time(int64_t chunks, int n) {  // in chunks of outputs, of the longest segment
+  return chunks * kStateShare / (1 - pow(1 - kStateShare, n));
+}
+
+// How many of those to use, or 0: where their time is less than that of the
+// launches they save (three bf16 chunks of outputs, half an fp32 one) and of the
+// form above.  That one / this, bf16: 16 heads of 509 tokens (d = 64) 12.6 / 10.4 us,
+// 32 of 512 (d = 128) 23.5 / 17.8, 128 of 509 (d = 64) 20.5 / 16.1, 96 of 1000 (d =
+// 128) 52.6 / 41.3, but 24 of 2045 (d = 128) 39 / 52.  Past 128 heads, with a segment each
+// in the form above, two or three: 240 of 1000 (d = 64) 44.1 / 37.0, 256 of 2000 72.3 /
+// 65.2.  Long sequences that get two workgroups a CU above keep them, but for
+// heads of 128 that get four segments there and two here (128 of 4093 190 / 170).
+int alone_of(int dtype, int64_t heads, int64_t L, int d) {
+  const int64_t chunks = (L + kChunk - 1) / kChunk;
+  const bool quick = dtype == ACID_BF16;
+  if (chunks < 2 || heads < 1) return 0;
+  if (heads > 128) {
+    if (chunks < (quick ? 3 : 8) || (!quick && d == 128)) return 0;
+    return heads <= 256 ? (int)(512 / heads) : quick && d == 64 && heads <= 384 ? 2 : 0;
+  }
+  const int64_t most = 256 / heads;
+  if (quick && heads * chunks >= 512 * 8) return d == 128 && 512 / heads <= 4 ? 2 : 0;
+  const int64_t apart = chunks > 2 ? chunks - 1 : 2;
+  const int n = (int)(most < apart ? most < kMaxAlone ? most : kMaxAlone
+                                   : apart < kMaxAlone ? apart : kMaxAlone);
+  int64_t per = (chunks + most - 1) / most;
+  if (quick && per == 1 && heads * chunks > 128) per = 2;
+  return alone_time(chunks, n) <= (quick ? 3 : 0.5) + (1 + kStateShare) * per ? n : 0;
+}
+
+// Where their segments begin, so that they end at the same time: segment j of c
+// chunks after C others takes r C + c, and what is before segment j + 1 is
+// C (1 - r) + that time.
+void cut_alone(int64_t chunks, int n, int32_t (&cut)[kMaxAlone - 1]) {
+  const double each = alone_time(chunks, n);
+  double c = 0;
+  for (int j = 0; j + 1 < n; ++j) {
+    c = c * (1 - kStateShare) + each;
+    const int64_t least = j ? cut[j - 1] / kChunk + 1 : 1, most = chunks - (n - 1 - j);
+    const int64_t at = (int64_t)(c + 0.5);
+    cut[j] = (int32_t)((at < least ? least : at > most ? most : at) * kChunk);
+  }
+}
+
 template <typename T, int D>
 hipError_t launch_chunks(const ChunkArgs& a, int64_t heads, hipStream_t s) {
-  if (a.segments > 1) {
+  if (a.slots) {
     hipLaunchKernelGGL((la_state_kernel<T, D>), dim3((unsigned)(heads * (a.segments - 1))),
                        dim3(4 * D), 0, s, a);
     if (a.scanned)
@@ -976,11 +1071,19 @@ extern "C" {
 
 size_t acid_linear_attention_workspace_bytes(int64_t n_seq, int32_t n_heads, int64_t seq_len,
                                              int32_t head_dim) {
-  if (check_heads(ACID_BF16, n_seq, n_heads, head_dim) != ACID_OK || seq_len < 0 ||
+  // (an fp32 call has no fewer segments than a bf16 one)
+  return acid_linear_attention_workspace_needed(ACID_F32, n_seq, n_heads, seq_len, head_dim, 1);
+}
+
+size_t acid_linear_attention_workspace_needed(int32_t dtype, int64_t n_seq, int32_t n_heads,
+                                              int64_t seq_len, int32_t head_dim,
+                                              int32_t in_place) {
+  if (check_heads(dtype, n_seq, n_heads, head_dim) != ACID_OK || seq_len < 0 ||
       seq_len > kMaxTokens)
     return 0;
   const int64_t heads = n_seq * n_heads;
-  const Segments seg = segments_of(ACID_F32, heads, seq_len);  // no fewer than in bf16
+  if (!in_place && alone_of(dtype, heads, seq_len, head_dim) > 1) return 0;
+  const Segments seg = segments_of(dtype, heads, seq_len);
   return seg.count > 1 ? (size_t)(seg.count * heads * head_dim * head_dim * 4) : 0;
 }
 
@@ -1021,8 +1124,12 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
   if (state_in_dev != state_out_dev &&
       bytes_overlap(state_in_dev, states, state_out_dev, states))
     return set_error(ACID_ERR_INVALID_ARG, "state_in and state_out: one buffer or apart");
-  const Segments seg = segments_of(dtype, heads, seq_len);
-  if (seg.count > 1) {
+  // (in place, a segment may end before another has read the state)
+  const bool in_place = state_in_dev && state_in_dev == state_out_dev;
+  const int alone = in_place ? 0 : alone_of(dtype, heads, seq_len, head_dim);
+  const Segments seg = alone > 1 ? Segments{0, alone} : segments_of(dtype, heads, seq_len);
+  const bool slots = alone <= 1 && seg.count > 1;
+  if (slots) {
     const int64_t need = seg.count * states;
     if ((int64_t)workspace_bytes < need || !workspace_dev)
       return set_error(ACID_ERR_SHAPE, "workspace of %lld bytes, %lld needed",
@@ -1037,10 +1144,11 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
   }
   StreamDevice on;
   ACID_TRY(on.enter(stream));
-  const ChunkArgs a = {q_dev, k_dev, vt_dev, o_dev, vt_ld, slopes_dev, lengths_dev, state_in_dev,
-                       state_out_dev, seg.count > 1 ? (float*)workspace_dev : nullptr, seq_len,
-                       n_heads, (int32_t)seg.count, (int32_t)seg.tokens,
-                       seg.count > most_folded(head_dim), scale};
+  ChunkArgs a = {q_dev, k_dev, vt_dev, o_dev, vt_ld, slopes_dev, lengths_dev, state_in_dev,
+                 state_out_dev, slots ? (float*)workspace_dev : nullptr, seq_len, n_heads,
+                 (int32_t)seg.count, (int32_t)seg.tokens, seg.count > most_folded(head_dim), {},
+                 scale};
+  if (alone > 1) cut_alone((seq_len + kChunk - 1) / kChunk, alone, a.cut);
   hipError_t e;
   if (dtype == ACID_BF16)
     e = head_dim == 64 ? launch_chunks<bf16, 64>(a, heads, stream)

@@ -143,6 +143,26 @@ def test_state_in_place_and_repeatable(dtype, L, d):
     assert torch.equal(a.o, c.o) and torch.equal(a.state_out, c.state_out)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("carried", [True, False])
+@pytest.mark.parametrize("n,heads,L,d,lengths", [
+    (1, 2, 65, 64, None), (2, 3, 128, 128, [127, 64]), (2, 2, 192, 64, [192, 0]), (3, 4, 320, 128, [320, 1, 65]),
+    (1, 40, 500, 64, None), (5, 20, 511, 128, [511, 256, 0, 129, 64]), (13, 10, 513, 64, [513 - 40 * i for i in range(13)]),
+    (4, 50, 260, 128, [260, 64, 0, 193])])
+def test_segments_that_make_their_own_states(dtype, carried, n, heads, L, d, lengths):
+    """With a state apart and in place, which shorter sequences take in
+    different ways."""
+    P = need_gpu()
+    p = Prompt(dtype, n, heads, L, d, lengths, carried=carried, seed=L).run(P)
+    p.check(what="apart")
+    if carried:
+        p.state_out, p.o = p.state.clone(), torch.full_like(p.o, 7.0)
+        p.state, first = p.state_out, p.state
+        p.run(P)
+        p.state = first
+        p.check(what="in place")
+
+
 def test_later_tokens_do_not_reach_earlier_outputs():
     P = need_gpu()
     a, b = (Prompt("bf16", 1, 2, 500, 128, seed=6) for _ in range(2))

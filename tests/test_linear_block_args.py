@@ -49,6 +49,22 @@ def test_attention_refuses_a_small_workspace(lib):
     assert lib.acid_linear_attention_workspace_bytes(1, 2, -1, 64) == 0
 
 
+def test_workspace_needed_is_no_more_than_enough(lib):
+    some = 0
+    for dtype in (L.ACID_BF16, L.ACID_F32):
+        for d in (64, 128):
+            for heads in (1, 2, 5, 8, 31, 64, 65, 86, 100, 128, 129, 171, 256, 257, 384, 385, 1000):
+                for tokens in (0, 1, 64, 65, 129, 300, 512, 1000, 3000, 5000, 40000, 1 << 28):
+                    enough = lib.acid_linear_attention_workspace_bytes(1, heads, tokens, d)
+                    in_place, apart = (lib.acid_linear_attention_workspace_needed(dtype, 1, heads, tokens, d, i)
+                                       for i in (1, 0))
+                    assert apart in (0, in_place) and in_place <= enough
+                    assert enough % (heads * d * d * 4) == 0 and enough <= 512 * d * d * 4
+                    some += apart < in_place
+    assert some > 50
+    assert lib.acid_linear_attention_workspace_needed(9, 1, 2, 40000, 128, 0) == 0
+
+
 def test_attention_of_no_sequences_does_nothing(lib):
     assert _attend(lib, n=0, q=None, k=None, vt=None, slopes=None, o=None, ws=None, bytes=0) == 0
 
