@@ -4,7 +4,7 @@
 //   out[m][n] = act(sum_k x[m][k] (c[n][k] - 8) s[n][k / group] + bias[n])
 //
 // Bound by reading the codes once (HBM: 28672 x 8192 with groups of 128, 125 MB, 8
-// bf16 rows, 27 us, 4.6 TB/s), so the layout is the one the matrix
+// bf16 rows, 25 us, 5.0 TB/s), so the layout is the one the matrix
 // instruction takes: a tile is 16 outputs x 128 inputs, 1 KB, and lane l of
 // the wave that reads it gets the 16 bytes of output l % 16 whose word j
 // holds inputs 32 j + 8 (l / 16) .. + 7, its share of the j-th 16x16x32
@@ -34,17 +34,14 @@ __device__ __forceinline__ bf16x8 decode(uint32_t w) {
 // fp32 row becomes three operand rows: the value cut to its first eight
 // significant bits, the next eight, and the rest; their sum is exact, and the
 // three products are added at the end.
-__device__ __forceinline__ bf16x8 load_x(const bf16* p, int) {
-  return *reinterpret_cast<const bf16x8*>(p);
-}
-__device__ __forceinline__ bf16x8 load_x(const float* p, int part) {
-  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+__device__ __forceinline__ bf16x8 operand(const bf16x8 (&v)[1], int) { return v[0]; }
+__device__ __forceinline__ bf16x8 operand(const f32x4 (&v)[2], int part) {
   const uint32_t less0 = part > 0 ? 0xffff0000u : 0u, less1 = part > 1 ? 0xffff0000u : 0u;
   uint32_t u[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float v = i < 4 ? a[i & 3] : b[i & 3];
-    const float r = v - __uint_as_float(__float_as_uint(v) & less0);
+    const float x = v[i / 4][i % 4];
+    const float r = x - __uint_as_float(__float_as_uint(x) & less0);
     u[i] = __float_as_uint(r - __uint_as_float(__float_as_uint(r) & less1));
   }
   u32x4 out;  // the upper halves
@@ -52,6 +49,48 @@ __device__ __forceinline__ bf16x8 load_x(const float* p, int part) {
   for (int i = 0; i < 4; ++i) out[i] = __builtin_amdgcn_perm(u[2 * i + 1], u[2 * i], 0x07060302u);
   return __builtin_bit_cast(bf16x8, out);
 }
+
+// The rows of one 128-input block, by way of a part of LDS that is one wave's
+// alone: loaded there as whole lines, 1 KB an instruction, read as the operands
+// they are.  (Each lane's own 16 bytes from L2, 64 of 16 rows an instruction: 16
+// rows of 2048 x 28672 30 us for 18, 32 of 8192 x 8192 20 for 15, one of 2048 x 28672
+// 12.6 for 13.7; fp32, 4 rows of 2048 x 28672 29 for 23, 64 of 8192 x 8192 81 for 84.)
+// The 16-byte chunk c of row r is at slot c ^ swizzle(r), so that the rows of one
+// chunk lie in different banks.
+template <typename X>
+struct Rows {
+  typedef std::conditional_t<std::is_same_v<X, float>, f32x4, bf16x8> Chunk;
+  static constexpr int CHUNKS = sizeof(X) * 8;     // of a row
+  static constexpr int EIGHT = sizeof(X) / 2;      // of eight inputs
+  static constexpr int PER_LOAD = 64 / CHUNKS;     // rows of an instruction
+  static constexpr int MOST = std::is_same_v<X, float> ? 5 : 16;  // rows of a row tile
+  static __host__ __device__ constexpr int loads(int rows) { return (rows + PER_LOAD - 1) / PER_LOAD; }
+  static __device__ __forceinline__ int swizzle(int r) { return EIGHT * r; }
+  // rows m0 .. of x (at input k0), `rows` of them
+  static __device__ __forceinline__ void load(const X* x, int64_t x_ld, int rows, uint32_t lds,
+                                              int lane) {
+    for (int i = 0; i < loads(rows); ++i) {
+      const int at = i * PER_LOAD + lane / CHUNKS, r = at < rows ? at : rows - 1;
+      const X* p = x + r * x_ld + (lane % CHUNKS ^ swizzle(at)) % CHUNKS * (16 / (int)sizeof(X));
+      asm volatile(
+          "s_mov_b32 m0, %1\n\t"
+          "s_nop 0\n\t"
+          "global_load_lds_dwordx4 %0, off"
+          :
+          : "v"(p), "s"(__builtin_amdgcn_readfirstlane(lds + i * 1024))
+          : "memory");
+    }
+  }
+  // inputs 32 j + 8 g .. + 7 of row r
+  static __device__ __forceinline__ void read(Chunk (&out)[EIGHT], uint32_t lds, int r, int j,
+                                              int g) {
+#pragma unroll
+    for (int e = 0; e < EIGHT; ++e) {
+      const int slot = (EIGHT * (4 * j + g) + e ^ swizzle(r)) % CHUNKS;
+      out[e] = *(const __attribute__((address_space(3))) Chunk*)(lds + (r * CHUNKS + slot) * 16);
+    }
+  }
+};
 
 struct W4Args {
   const void* x;
@@ -63,8 +102,8 @@ struct W4Args {
   int32_t M, N, K, gelu;
 };
 
-// Sixteen waves pay where few tiles meet many blocks: 1536 x 8960, one row, 6.4 ->
-// 5.6 us (of 1536 inputs, twelve waves to eight: 3.7 -> 4.1).
+// Sixteen waves pay where few tiles meet many blocks: 1536 x 8960, one row, 8 / 16
+// waves 7.0 / 6.3 us (4608 x 1536, 8 / 12 waves: 4.0 / 4.3).
 template <int NT, int MT>
 constexpr int MOST_WAVES = NT * MT == 1 ? 16 : 8;
 
@@ -75,20 +114,25 @@ constexpr int MOST_WAVES = NT * MT == 1 ? 16 : 8;
 // the group's scale.
 template <typename X, typename Out, int GROUP, int NT, int MT>
 __global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4Args a) {
-  constexpr int RPT = std::is_same_v<X, float> ? 5 : 16;  // rows of a row tile
-  extern __shared__ float red[];                          // [wave][mt][nt][16][16]
+  typedef Rows<X> R;
+  constexpr int RPT = R::MOST;
+  extern __shared__ __align__(1024) float red[];  // the rows; then sums, [wave][mt][nt][16][16]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int col = lane & 15, g = lane >> 4;
   const int KB = a.K / 128, tiles = (a.N + 15) / 16;
   const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * (MT * RPT);
   const int part = std::is_same_v<X, float> ? col % 3 : 0;
 
-  const X* x[MT];
+  // operand row col: of row `row` of the tile; past the end a copy whose result is dropped
+  const int row = std::is_same_v<X, float> ? (col < 15 ? col / 3 : 4) : col;
+  const int loads = R::loads(a.M < RPT ? a.M : RPT);  // of a row tile
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)red +
+                       wave * (MT * loads * 1024);
+  int rows[MT];
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
-    int m = m0 + mt * RPT + (std::is_same_v<X, float> ? (col < 15 ? col / 3 : 4) : col);
-    m = m < a.M ? m : a.M - 1;  // rows past the end: copies whose results are dropped
-    x[mt] = (const X*)a.x + m * a.x_ld + 8 * g;
+    const int left = a.M - m0 - mt * RPT;
+    rows[mt] = left < RPT ? left : RPT;
   }
   const u32x4* codes[NT];
   const float* scales[NT];
@@ -108,10 +152,15 @@ __global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) acc[mt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // a block's codes and scales, one block ahead of the products
+  // a block's rows, codes and scales, one block ahead of the products
   u32x4 c_next[NT];
   float s_next[NT][128 / GROUP];
   auto load = [&](int b) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+      if (rows[mt] > 0)
+        R::load((const X*)a.x + (int64_t)(m0 + mt * RPT) * a.x_ld + b * 128, a.x_ld, rows[mt],
+                lds + mt * loads * 1024, lane);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       c_next[nt] = codes[nt][b * 64];
@@ -122,11 +171,18 @@ __global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4
   };
   load(wave);  // there are no more waves than blocks
   for (int b = wave; b < KB; b += waves) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     bf16x8 xf[MT][4];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) xf[mt][j] = load_x(x[mt] + b * 128 + 32 * j, part);
+      for (int j = 0; j < 4; ++j) {
+        typename R::Chunk v[R::EIGHT];
+        const int r = row < rows[mt] ? row : rows[mt] > 0 ? rows[mt] - 1 : 0;
+        R::read(v, lds + mt * loads * 1024, r, j, g);
+        xf[mt][j] = operand(v, part);
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     u32x4 c[NT];
     float s[NT][128 / GROUP];
 #pragma unroll
@@ -161,6 +217,7 @@ __global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4
       }
     }
   }
+  __syncthreads();  // the rows have been read
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -194,29 +251,31 @@ __global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4
 
 template <typename X, typename Out, int GROUP>
 hipError_t launch(const W4Args& a, hipStream_t s) {
-  constexpr int RPT = std::is_same_v<X, float> ? 5 : 16;
+  constexpr int RPT = Rows<X>::MOST;
   const int tiles = (a.N + 15) / 16, KB = a.K / 128;
+  const int loads = Rows<X>::loads(a.M < RPT ? a.M : RPT);
 #define W4(NT, MT)                                                                            \
   do {                                                                                        \
     const int waves = KB < 8 ? KB : KB < 32 ? 8 : MOST_WAVES<NT, MT>;                         \
     hipLaunchKernelGGL((linear_w4_kernel<X, Out, GROUP, NT, MT>),                             \
                        dim3((tiles + NT - 1) / NT, (a.M + MT * RPT - 1) / (MT * RPT)),        \
-                       dim3(64 * waves), waves * NT * MT * 1024, s, a);                       \
+                       dim3(64 * waves), waves * MT * (loads > NT ? loads : NT) * 1024, s, a);            \
   } while (0)
   // Two row tiles at once where there are two, so that codes are read and
-  // decoded once for both.  Output tiles: as many as leave a workgroup for each
-  // CU, since each reads the rows (4 KB a block and row tile, to 1 KB of codes
-  // an output tile).  28672 x 8192, bf16 rows, 1 / 16 / 32 of them: 27 / 31 / 45 us
-  // with four output tiles; 8192 x 28672: 30 / 58 / 72 with one (two of 32), 30 /
-  // 35 / 61 with two (four of 32).  Four row tiles ran slower than two and two.
-  const int most = tiles * ((a.M + 2 * RPT - 1) / (2 * RPT)) / 256;
+  // decoded once for both.  Output tiles: as many as leave a workgroup for seven
+  // CUs in eight, since each reads the rows (4 KB a block and row tile, to 1 KB of
+  // codes an output tile).  1 / 16 / 32 bf16 rows: 28672 x 8192 26 / 35 / 55 us with one
+  // output tile, 25 / 27 / 38 with four; 8192 x 28672 (512 tiles) 23 / 34 / 57 with one,
+  // 22 / 29 / 41 with two, 34 / 40 / 55 with four; 14336 x 4096 (896) 8.4 / 10.2 / 14.9 with
+  // two, 8.6 / 9.8 / 12.7 with four.  Four row tiles ran slower than two and two.
+  const int groups = tiles * ((a.M + 2 * RPT - 1) / (2 * RPT));
   if (a.M <= RPT) {
-    if (most >= 4) W4(4, 1);
-    else if (most >= 2) W4(2, 1);
+    if (groups >= 4 * 224) W4(4, 1);
+    else if (groups >= 2 * 224) W4(2, 1);
     else W4(1, 1);
   } else {
-    if (most >= 4) W4(4, 2);
-    else if (most >= 2) W4(2, 2);
+    if (groups >= 4 * 224) W4(4, 2);
+    else if (groups >= 2 * 224) W4(2, 2);
     else W4(1, 2);
   }
 #undef W4
