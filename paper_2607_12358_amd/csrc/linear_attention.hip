@@ -1124,6 +1124,13 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
   if (state_in_dev != state_out_dev &&
       bytes_overlap(state_in_dev, states, state_out_dev, states))
     return set_error(ACID_ERR_INVALID_ARG, "state_in and state_out: one buffer or apart");
+  const struct {
+    const void* p;
+    int64_t bytes;
+  } small[] = {{slopes_dev, n_heads * (int64_t)4}, {lengths_dev, n_seq * 4}};
+  for (const auto& v : small)
+    if (bytes_overlap(o_dev, qkv, v.p, v.bytes) || bytes_overlap(state_out_dev, states, v.p, v.bytes))
+      return set_error(ACID_ERR_INVALID_ARG, "o or state_out overlaps the slopes or the lengths");
   // (in place, a segment may end before another has read the state)
   const bool in_place = state_in_dev && state_in_dev == state_out_dev;
   const int alone = in_place ? 0 : alone_of(dtype, heads, seq_len, head_dim);
@@ -1141,6 +1148,9 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
         bytes_overlap(workspace_dev, need, state_in_dev, states) ||
         bytes_overlap(workspace_dev, need, state_out_dev, states))
       return set_error(ACID_ERR_INVALID_ARG, "the workspace overlaps vt or a state");
+    for (const auto& v : small)
+      if (bytes_overlap(workspace_dev, need, v.p, v.bytes))
+        return set_error(ACID_ERR_INVALID_ARG, "the workspace overlaps the slopes or the lengths");
   }
   StreamDevice on;
   ACID_TRY(on.enter(stream));
@@ -1199,6 +1209,14 @@ acid_status acid_linear_attention_step(int32_t dtype, int64_t n_rows, int32_t n_
   if (rows_overlap(state_in_dev, 1, states, states, o_dev, n_rows, w, o_ld * size) ||
       rows_overlap(state_out_dev, 1, states, states, o_dev, n_rows, w, o_ld * size))
     return set_error(ACID_ERR_INVALID_ARG, "o overlaps a state");
+  const struct {
+    const void* p;
+    int64_t bytes;
+  } small[] = {{slopes_dev, n_heads * (int64_t)4}, {slots_dev, n_rows * 4}};
+  for (const auto& v : small)
+    if (rows_overlap(o_dev, n_rows, w, o_ld * size, v.p, 1, v.bytes, v.bytes) ||
+        bytes_overlap(state_out_dev, states, v.p, v.bytes))
+      return set_error(ACID_ERR_INVALID_ARG, "o or state_out overlaps the slopes or the slots");
   if (state_in_dev != state_out_dev &&
       bytes_overlap(state_in_dev, states, state_out_dev, states))
     return set_error(ACID_ERR_INVALID_ARG, "state_in and state_out: one buffer or apart");
