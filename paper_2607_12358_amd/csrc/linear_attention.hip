@@ -15,6 +15,29 @@
 namespace acid {
 namespace {
 
+// A value that is the same in every lane, kept in a scalar register.
+__device__ __forceinline__ float uniform(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+
+// exp(-slope n), the decay over n tokens, as a sum of two fp32 values: a factor
+// rounded once is off to the same side each time it is applied, and that adds
+// up over a state's memory (one rounded factor a token, slope 1e-4, 8192 tokens:
+// 1.8e-4 of the state).
+struct Decay {
+  float hi, lo;
+  __device__ __forceinline__ Decay(float slope, double n) {
+    const double w = exp(-(double)slope * n);
+    hi = uniform((float)w);
+    lo = uniform((float)(w - (double)hi));
+  }
+  __device__ __forceinline__ float operator()(float x) const { return fmaf(x, hi, x * lo); }
+  // decayed x + y
+  __device__ __forceinline__ float operator()(float x, float y) const {
+    return fmaf(x, hi, fmaf(x, lo, y));
+  }
+};
+
 struct StepArgs {
   const void *q, *k, *v;
   void* o;
@@ -82,12 +105,12 @@ __global__ __launch_bounds__(256) void la_step_kernel(StepArgs a) {
   const T* v = (const T*)a.v + head * D + slice * 32 + cg * 4;
   T* o = (T*)a.o + head * D + slice * 32;
   const int64_t at = (slot * a.heads + head) * (D * D) + slice * 32 + cg * 4;
-  const float lambda = expf(-a.slopes[head]);
 
   float4 s[R];
 #pragma unroll
   for (int i = 0; i < R; ++i)
     s[i] = *reinterpret_cast<const float4*>(a.state_in + at + (rg + 32 * i) * D);
+  const Decay decay(a.slopes[head], 1.0);
   int parity = 0;
   for (int64_t t = row; t >= 0;
        t = a.slots ? find_slot(a.slots, (int32_t)slot, t + 1, a.rows) : -1) {
@@ -98,10 +121,10 @@ __global__ __launch_bounds__(256) void la_step_kernel(StepArgs a) {
     for (int i = 0; i < R; ++i) {
       const float kt = (float)k[t * a.k_ld + rg + 32 * i];
       const float qt = (float)q[t * a.q_ld + rg + 32 * i];
-      s[i].x = lambda * s[i].x + kt * vt.x;
-      s[i].y = lambda * s[i].y + kt * vt.y;
-      s[i].z = lambda * s[i].z + kt * vt.z;
-      s[i].w = lambda * s[i].w + kt * vt.w;
+      s[i].x = decay(s[i].x, kt * vt.x);
+      s[i].y = decay(s[i].y, kt * vt.y);
+      s[i].z = decay(s[i].z, kt * vt.z);
+      s[i].w = decay(s[i].w, kt * vt.w);
       y.x += qt * s[i].x;
       y.y += qt * s[i].y;
       y.z += qt * s[i].z;
@@ -232,11 +255,6 @@ __device__ __forceinline__ f32x4 mma(const Operand<float>& a, const Operand<floa
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// A value that is the same in every lane, kept in a scalar register.
-__device__ __forceinline__ float uniform(float x) {
-  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
-}
 
 // log2(e) slope: the decay over n tokens is exp2(-rate n).  Capped, so that an
 // infinite slope still gives 1 over no tokens.
