@@ -26,8 +26,8 @@ __device__ __forceinline__ float uniform(float x) {
 // 1.8e-4 of the state).
 struct Decay {
   float hi, lo;
-  __device__ __forceinline__ Decay(float slope, double n) {
-    const double w = exp(-(double)slope * n);
+  __device__ __forceinline__ Decay(float slope, double n) : Decay(exp(-(double)slope * n)) {}
+  __device__ __forceinline__ explicit Decay(double w) {
     hi = uniform((float)w);
     lo = uniform((float)(w - (double)hi));
   }
@@ -583,6 +583,14 @@ __device__ __forceinline__ void write_state(State<D>& s, float* p) {
   });
 }
 
+template <int D>
+__device__ __forceinline__ void fade(State<D>& s, const Decay& decay) {
+  for_state(s, [&](f32x4& t, int, int, int) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = decay(t[i]);
+  });
+}
+
 // Where there are too few heads to fill the chip, a sequence is cut into
 // segments.  This kernel leaves in slot j + 1 what segment j adds to the state
 // (segment 0: what it makes of state_in), for each segment that another
@@ -610,8 +618,7 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_state_kernel
   const float rate = decay_rate(a.slopes[head]);
   const Powers pw(rate);
   if (seg == 0 && a.state_in) {
-    const float w = (float)exp(-(double)a.slopes[head] * a.segment);
-    for_state(s, [&](f32x4& t, int, int, int) { t *= w; });
+    fade(s, Decay(a.slopes[head], a.segment));
   } else {
     for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{0.f, 0.f, 0.f, 0.f}; });
   }
@@ -733,13 +740,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
   const T* vt = (const T*)a.vt + (hs * D + wave * 16) * a.vt_ld;
   const int64_t o_ld = (int64_t)a.heads * D;
   T* o = (T*)a.o + seq * a.tokens * o_ld + head * D + wave * 16;
-  // lambda^64, for a state in fp32 in two parts: a rounded factor would add up
-  // over the chunks
-  constexpr bool TWO_PART_DECAY = LAST || sizeof(T) == 4;
-  const double whole = exp(-(double)slope * kChunk);
   const Powers pw(rate);
-  const float whole_hi = uniform((float)whole);
-  const float whole_lo = uniform((float)(whole - (double)whole_hi));
   // LDS: K's rows of this chunk and the next, Q's, V's (each wave its own),
   // the scores.  Q and V have one place each: the next chunk's are loaded once
   // all that is in it has been read.
@@ -781,8 +782,7 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     V::load(vt, a.vt_ld, kChunk, v_now, lane);
     if (a.state_in) {
       read_state(s, a.state_in + hs * (D * D));
-      const float w = (float)exp(-(double)slope * begin);
-      for_state(s, [&](f32x4& t, int, int, int) { t *= w; });
+      fade(s, Decay(slope, (double)begin));
     } else {
       for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{0.f, 0.f, 0.f, 0.f}; });
     }
@@ -816,14 +816,24 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     for_state(s, [&](f32x4& t, int at, int, int) {
       t = *reinterpret_cast<const f32x4*>(slot + at);
     });
-    if (!a.scanned)  // the segments before the last one, each with its decay
-      for (int j = 1; j < seg; ++j) {
-        const float w = exp2_fast(-rate * (float)((seg - j) * a.segment));
+    if (!a.scanned) {  // the segments before the last one, each with its decay
+      const double step = exp(-(double)slope * a.segment);
+      double w = step;
+      for (int j = seg - 1; j > 0; --j, w *= step) {
+        const Decay decay(w);
         for_state(s, [&](f32x4& t, int at, int, int) {
-          t += w * *reinterpret_cast<const f32x4*>(slot - (int64_t)(seg - j) * (D * D) + at);
+          const f32x4 x = *reinterpret_cast<const f32x4*>(slot - (int64_t)(seg - j) * (D * D) + at);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) t[i] = decay(x[i], t[i]);
         });
       }
+    }
   }
+  // (made while the loads above are on their way)  Over a chunk, and over the ragged
+  // one at a sequence's end; for a state that is only read by a segment's own bf16
+  // outputs one part will do.
+  constexpr bool TWO_PART_DECAY = LAST || sizeof(T) == 4;
+  const Decay whole(slope, kChunk), ragged(slope, (int)(end - begin) & (kChunk - 1));
   float tile_decay[4];
 #pragma unroll
   for (int tt = 0; tt < 4; ++tt) tile_decay[tt] = uniform(a.scale * exp2_fast(-rate * (float)(16 * tt)));
@@ -930,16 +940,9 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
       at += 16 * o_ld;
     }
     if (update) {
-      if constexpr (WHOLE)
-        for_state(s, [&](f32x4& t, int, int, int) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            t[i] = TWO_PART_DECAY ? fmaf(t[i], whole_hi, t[i] * whole_lo) : t[i] * whole_hi;
-        });
-      else {
-        const float w = exp2_fast(-rate * (float)n);
-        for_state(s, [&](f32x4& t, int, int, int) { t *= w; });
-      }
+      if constexpr (!WHOLE) fade(s, ragged);
+      else if constexpr (TWO_PART_DECAY) fade(s, whole);
+      else for_state(s, [&](f32x4& t, int, int, int) { t *= whole.hi; });
       add_outer<T, D, PARTS, WHOLE>(s, afresh(buf + column_base<T, D>(lane)), v, rate,
                                     pw, n - 1, lane);
     }

@@ -61,3 +61,50 @@ def test_tokens_one_by_one(fading):
     P.linear_attention_step(rows[0], rows[0], rows[1], torch.tensor(SLOPES, device="cuda"), o, pool,
                             slots=torch.zeros(n, dtype=torch.int32, device="cuda"))
     _check(pool[0], k, v, state, n, n, f"steps, {'fading' if fading else 'growing'}")
+
+
+# (dtype, tokens a call, head_dim, in place, roundings of a fading state's value a call): one chunk or
+# two, segments whose states the outputs' kernel adds, segments that are scanned, segments that
+# each make their own state
+STREAMS = [("bf16", 1, 64, True, 1), ("f32", 1, 128, True, 1), ("bf16", 17, 128, True, 1), ("f32", 40, 64, True, 1),
+           ("bf16", 65, 64, True, 2), ("f32", 300, 64, True, 3), ("f32", 700, 128, True, 3),
+           ("bf16", 700, 64, True, 3), ("bf16", 300, 64, False, 4)]
+
+
+@pytest.mark.parametrize("dtype,L,d,in_place,roundings", STREAMS)
+def test_stream_of_prompts(dtype, L, d, in_place, roundings):
+    """400 calls of L tokens with k = 0, each from the state before; slopes for
+    which exp(-slope L) lies far from the fp32 values beside it."""
+    P = need_gpu()
+    calls, each = 400, 4
+    slopes = []
+    for i in range(1000):
+        slope = float(np.float32(1e-4 + 1e-7 * i))
+        f = (float(np.float32(math.exp(-slope * L))) / math.exp(-slope * L) - 1) / U
+        if abs(f) > 0.42 and len(slopes) < 3:
+            slopes.append(slope)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    heads = each * len(slopes)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(L)
+    state = 0.5 + torch.rand((heads, d, d), generator=g, device="cuda")
+    q, k = (torch.zeros((heads, L, d), dtype=dt, device="cuda") for _ in range(2))
+    vt = torch.ones((heads, d, (L + 7) // 8 * 8), dtype=dt, device="cuda")
+    sl = torch.tensor(np.repeat(slopes, each), dtype=torch.float32, device="cuda")
+    o = torch.empty((L, heads * d), dtype=dt, device="cuda")
+    now, then = state.clone(), torch.empty_like(state)
+    for _ in range(calls):
+        if in_place:
+            P.linear_attention(q, k, vt, sl, o, state_in=now, state_out=now)
+        else:
+            P.linear_attention(q, k, vt, sl, o, state_in=now, state_out=then)
+            now, then = then, now
+    for i, slope in enumerate(slopes):
+        part = slice(i * each, (i + 1) * each)
+        want = math.exp(-slope * L * calls) * state[part].double().cpu().numpy()
+        off = now[part].double().cpu().numpy() / want - 1
+        bound = (roundings * calls + 4) * U
+        mean = math.sqrt(2 * math.log(2e9) / off.size) * bound
+        print(f"{dtype} {L} tokens, slope {slope:.3e}: mean / bound {off.mean() / mean:.3f}, "
+              f"worst / bound {np.abs(off).max() / bound:.3f}", flush=True)
+        assert np.abs(off).max() <= bound and abs(off.mean()) <= mean, slope
