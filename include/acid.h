@@ -468,9 +468,10 @@ acid_status acid_block_forward(acid_model* m, int32_t block,
  * sequence b has lengths[b] tokens, clamped to [0, L]; what the padding holds
  * is never used, its rows of o are left as they are, and the state is the
  * one after the last token (state_in, or 0, for none).  d is 64 or 128.
- * Products are accumulated, and states kept, in fp32.  q, k, v and the state
- * must be finite: a NaN or an infinity spoils its head's outputs from 63
- * tokens before it on.
+ * Products are accumulated, and states kept, in fp32.  A NaN or an infinity in
+ * a token's q makes that token's outputs of the head NaN or infinite, one in k the
+ * head's outputs and a row of its state from that token on, one in v a column of
+ * both; nothing before the token is touched.
  * Workspace: acid_linear_attention_workspace_needed(...) bytes (0: may be
  * NULL), 16-byte aligned, not shared by calls that may overlap; ACID_ERR_SHAPE
  * if it is smaller.  in_place: state_out is state_in; a state apart lets shorter

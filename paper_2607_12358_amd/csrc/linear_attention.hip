@@ -6,6 +6,7 @@
 // S is fp32 [d][d] (rows over k's columns, columns over v's).  Both forms move
 // little more than they must: a token costs 4 d^2 operations a head for 4 d
 // values, a single token reads and writes its states.
+#include <float.h>
 #include <math.h>
 
 #include <type_traits>
@@ -244,6 +245,26 @@ __device__ __forceinline__ void keep_first(Operand<float>& x, int n) {
     x.b[e] = e + 4 < n ? x.b[e] : 0.f;
   }
 }
+__device__ __forceinline__ float sum8(const Operand<bf16>& x) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    s = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){x.v[2 * i], x.v[2 * i + 1]},
+                                        (bf16x2){(bf16)1.0f, (bf16)1.0f}, s, false);
+  return s;
+}
+__device__ __forceinline__ float sum8(const Operand<float>& x) {
+  const f32x4 s = x.a + x.b;
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+__device__ __forceinline__ bool finite(const Operand<bf16>& x, int e) {
+  return fabsf((float)x.v[e]) <= FLT_MAX;
+}
+__device__ __forceinline__ bool finite(const Operand<float>& x, int e) {
+  return fabsf(e < 4 ? x.a[e & 3] : x.b[e & 3]) <= FLT_MAX;
+}
+__device__ __forceinline__ void clear(Operand<bf16>& x, int e) { x.v[e] = (bf16)0.0f; }
+__device__ __forceinline__ void clear(Operand<float>& x, int e) { (e < 4 ? x.a : x.b)[e & 3] = 0.f; }
 __device__ __forceinline__ f32x4 mma(const Operand<bf16>& a, const Operand<bf16>& b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
 }
@@ -444,6 +465,29 @@ struct ValueTile {
   __device__ __forceinline__ void mask(int n, int lane) {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) keep_first(v[ks], n - 32 * ks - 8 * (lane >> 4));
+  }
+  // Whether any value of the wave's may be a NaN or an infinity: their sum is not finite.
+  __device__ __forceinline__ bool spoilt() const {
+    return __ballot(!(fabsf(sum8(v[0]) + sum8(v[1])) <= FLT_MAX)) != 0;
+  }
+  // The first token of the lane's column that is a NaN or an infinity (kChunk:
+  // none); all such become zeros.
+  __device__ __forceinline__ int take_spoilt(int lane) {
+    int first = kChunk;
+#pragma unroll
+    for (int ks = 1; ks >= 0; --ks)
+#pragma unroll
+      for (int e = 7; e >= 0; --e)
+        if (!finite(v[ks], e)) {
+          first = 32 * ks + 8 * (lane >> 4) + e;
+          clear(v[ks], e);
+        }
+#pragma unroll
+    for (int m = 16; m < 64; m <<= 1) {
+      const int other = __shfl_xor(first, m, 64);
+      first = first < other ? first : other;
+    }
+    return first;
   }
 };
 
@@ -920,6 +964,21 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
     for (int tt = 0; tt < 4; ++tt) out[tt] *= exp2_fast(-rate * (float)(col + 1)) * tile_decay[tt];
     barrier_lds();
     if (more) load_q(c0 + kChunk, lane);
+    // A NaN or an infinity among V's tokens would reach the chunk's earlier outputs
+    // too, whose weights for it are zeros: it is left out of V, and what comes of it is
+    // a NaN in its column of S and in the outputs from its token on.
+    if (__builtin_expect(v.spoilt(), 0)) {
+      const float nan = __builtin_nanf("");
+      const int first = v.take_spoilt(lane);
+      if (first < kChunk) for_state(s, [&](f32x4& t, int, int, int) { t = f32x4{nan, nan, nan, nan}; });
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int from = __shfl(first, 4 * g + i, 64);
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt)
+          if (16 * tt + (int)col >= from) out[tt][i] = nan;
+      }
+    }
 
     const uint32_t weights = afresh(scores + P::at(col, 8 * g));
 #pragma unroll
