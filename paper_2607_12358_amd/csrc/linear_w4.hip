@@ -53,8 +53,8 @@ __device__ __forceinline__ bf16x8 operand(const f32x4 (&v)[2], int part) {
 // The rows of one 128-input block, by way of a part of LDS that is one wave's
 // alone: loaded there as whole lines, 1 KB an instruction, read as the operands
 // they are.  (Each lane's own 16 bytes from L2, 64 of 16 rows an instruction: 16
-// rows of 2048 x 28672 30 us for 18, 32 of 8192 x 8192 20 for 15, one of 2048 x 28672
-// 12.6 for 13.7; fp32, 4 rows of 2048 x 28672 29 for 23, 64 of 8192 x 8192 81 for 84.)
+// rows of 2048 x 28672 30 us for 18, 32 of 8192 x 8192 20 for 15; fp32, 4 rows of 2048
+// x 28672 29 for 23, 32 of 1536 x 8960 32 for 28, but 64 of 8192 x 8192 83 for 86.)
 // The 16-byte chunk c of row r is at slot c ^ swizzle(r), so that the rows of one
 // chunk lie in different banks.
 template <typename X>
@@ -111,9 +111,10 @@ constexpr int MOST_WAVES = NT * MT == 1 ? 16 : 8;
 // waves take the 128-input blocks in turn and their sums are added in wave
 // order.  The matrix products give sum x (16 + c); one more product with the
 // constant -24, shared by the output tiles, makes that sum x (c - 8) before
-// the group's scale.
-template <typename X, typename Out, int GROUP, int NT, int MT>
-__global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4Args a) {
+// the group's scale.  ONE: x is one bf16 row, each lane reads its operand itself.
+template <typename X, typename Out, int GROUP, int NT, int MT, bool ONE>
+__device__ __forceinline__ void products(const W4Args& a) {
+  static_assert(!ONE || (std::is_same_v<X, bf16> && MT == 1), "one bf16 row");
   typedef Rows<X> R;
   constexpr int RPT = R::MOST;
   extern __shared__ __align__(1024) float red[];  // the rows; then sums, [wave][mt][nt][16][16]
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4
   auto load = [&](int b) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
-      if (rows[mt] > 0)
+      if (!ONE && rows[mt] > 0)
         R::load((const X*)a.x + (int64_t)(m0 + mt * RPT) * a.x_ld + b * 128, a.x_ld, rows[mt],
                 lds + mt * loads * 1024, lane);
 #pragma unroll
@@ -171,18 +172,24 @@ __global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4
   };
   load(wave);  // there are no more waves than blocks
   for (int b = wave; b < KB; b += waves) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     bf16x8 xf[MT][4];
+    if constexpr (ONE) {
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+      for (int j = 0; j < 4; ++j)
+        xf[0][j] = *reinterpret_cast<const bf16x8*>((const X*)a.x + b * 128 + 32 * j + 8 * g);
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        typename R::Chunk v[R::EIGHT];
-        const int r = row < rows[mt] ? row : rows[mt] > 0 ? rows[mt] - 1 : 0;
-        R::read(v, lds + mt * loads * 1024, r, j, g);
-        xf[mt][j] = operand(v, part);
-      }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          typename R::Chunk v[R::EIGHT];
+          const int r = row < rows[mt] ? row : rows[mt] > 0 ? rows[mt] - 1 : 0;
+          R::read(v, lds + mt * loads * 1024, r, j, g);
+          xf[mt][j] = operand(v, part);
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
     u32x4 c[NT];
     float s[NT][128 / GROUP];
 #pragma unroll
@@ -249,17 +256,27 @@ __global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4
   }
 }
 
+template <typename X, typename Out, int GROUP, int NT, int MT>
+__global__ __launch_bounds__(64 * (MOST_WAVES<NT, MT>)) void linear_w4_kernel(W4Args a) {
+  products<X, Out, GROUP, NT, MT, false>(a);
+}
+template <typename Out, int GROUP>
+__global__ __launch_bounds__(64 * (MOST_WAVES<1, 1>)) void linear_w4_row_kernel(W4Args a) {
+  products<bf16, Out, GROUP, 1, 1, true>(a);
+}
+
 template <typename X, typename Out, int GROUP>
 hipError_t launch(const W4Args& a, hipStream_t s) {
   constexpr int RPT = Rows<X>::MOST;
   const int tiles = (a.N + 15) / 16, KB = a.K / 128;
   const int loads = Rows<X>::loads(a.M < RPT ? a.M : RPT);
-#define W4(NT, MT)                                                                            \
+#define W4(NT, MT) W4_AS((linear_w4_kernel<X, Out, GROUP, NT, MT>), NT, MT)
+#define W4_AS(KERNEL, NT, MT)                                                                 \
   do {                                                                                        \
     const int waves = KB < 8 ? KB : KB < 32 ? 8 : MOST_WAVES<NT, MT>;                         \
-    hipLaunchKernelGGL((linear_w4_kernel<X, Out, GROUP, NT, MT>),                             \
+    hipLaunchKernelGGL(KERNEL,                                                                \
                        dim3((tiles + NT - 1) / NT, (a.M + MT * RPT - 1) / (MT * RPT)),        \
-                       dim3(64 * waves), waves * MT * (loads > NT ? loads : NT) * 1024, s, a);            \
+                       dim3(64 * waves), waves * MT * (loads > NT ? loads : NT) * 1024, s, a); \
   } while (0)
   // Two row tiles at once where there are two, so that codes are read and
   // decoded once for both.  Output tiles: as many as leave a workgroup for seven
@@ -269,6 +286,17 @@ hipError_t launch(const W4Args& a, hipStream_t s) {
   // 22 / 29 / 41 with two, 34 / 40 / 55 with four; 14336 x 4096 (896) 8.4 / 10.2 / 14.9 with
   // two, 8.6 / 9.8 / 12.7 with four.  Four row tiles ran slower than two and two.
   const int groups = tiles * ((a.M + 2 * RPT - 1) / (2 * RPT));
+  // One bf16 row has no lines to make whole, and where a CU has a workgroup at most
+  // nothing hides a second trip.  By way of LDS / past it: 2048 x 28672 13.8 / 12.6 us,
+  // 4096 x 14336 9.0 / 8.5, 1536 x 8960 6.2 / 5.9, 1024 x 2048 3.4 / 3.2, but 5000 x
+  // 14336 (313 tiles) 14.6 / 16.5, 8960 x 1536 5.1 / 5.2, two rows of 2048 x 28672
+  // 15.1 / 15.7, and groups of 64 and 32 of it 15.3 / 16.4 and 17.3 / 18.4.
+  if constexpr (std::is_same_v<X, bf16> && GROUP == 128) {
+    if (a.M == 1 && tiles <= 256) {
+      W4_AS((linear_w4_row_kernel<Out, GROUP>), 1, 1);
+      return hipGetLastError();
+    }
+  }
   if (a.M <= RPT) {
     if (groups >= 4 * 224) W4(4, 1);
     else if (groups >= 2 * 224) W4(2, 1);
@@ -279,6 +307,7 @@ hipError_t launch(const W4Args& a, hipStream_t s) {
     else W4(1, 2);
   }
 #undef W4
+#undef W4_AS
   return hipGetLastError();
 }
 
