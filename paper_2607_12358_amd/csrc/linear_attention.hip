@@ -517,7 +517,8 @@ __device__ __forceinline__ bf16x2 cut(float x0, float x1) {
 }
 
 // V times the tokens' decays, as operands whose sum it is: each product cut
-// to its first eight significant bits, the next eight, the rest.
+// to its first eight significant bits, the next eight, the rest.  The last of two is
+// rounded, since what is cut off would all be of one side (5e-6 of a long prompt's outputs).
 template <int PARTS>
 __device__ __forceinline__ void decayed(const Operand<bf16>& v, const float (&w)[8],
                                         Operand<bf16> (&out)[PARTS]) {
@@ -526,7 +527,7 @@ __device__ __forceinline__ void decayed(const Operand<bf16>& v, const float (&w)
     float x0 = (float)v.v[2 * i] * w[2 * i], x1 = (float)v.v[2 * i + 1] * w[2 * i + 1];
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) {
-      const bf16x2 c = cut(x0, x1);
+      const bf16x2 c = PARTS == 2 && p == 1 ? rounded(x0, x1) : cut(x0, x1);
       out[p].v[2 * i] = c[0];
       out[p].v[2 * i + 1] = c[1];
       if (p + 1 < PARTS) {
