@@ -261,6 +261,10 @@ def _on(torch, dev, stream, fn, *args) -> None:
         check(status)
 
 
+def _scale(d: int) -> float:
+    return d ** -0.5 if d else 1.0  # (no heads of 0: the library says so)
+
+
 def linear_attention_workspace(n_seq: int, n_heads: int, seq_len: int, head_dim: int) -> int:
     """Bytes of workspace that are enough for linear_attention of these sizes."""
     return int(lib().acid_linear_attention_workspace_bytes(n_seq, n_heads, seq_len, head_dim))
@@ -293,7 +297,7 @@ def linear_attention(q, k, vt, slopes, o, state_in=None, state_out=None, lengths
             at(dev, "lengths", lengths, (n_seq,), torch.int32),
             at(dev, "state_in", state_in, states, torch.float32),
             at(dev, "state_out", state_out, states, torch.float32),
-            d ** -0.5 if scale is None else scale,
+            _scale(d) if scale is None else scale,
             at(dev, "o", o, lead + (L, n_heads * d), dt))
     if workspace is None:
         in_place = args[6] is not None and args[6] == args[7]
@@ -318,6 +322,8 @@ def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
     torch, N, at, rows_at = _native()
     if state.dim() != 4:
         raise ValueError("state: expected [n_slots, heads, d, d]")
+    if q.dim() != 2:
+        raise ValueError("q: expected [rows, heads*d]")
     code, dev, dt = _dtype_code(torch, q, "q"), _device(state, "state"), q.dtype
     n_slots, n_heads, d = state.shape[:3]
     rows, states = q.shape[0], (n_slots, n_heads, d, d)
@@ -328,7 +334,7 @@ def linear_attention_step(q, k, v, slopes, o, state, state_out=None, slots=None,
         *rows_at(dev, "v", v, shape, dt), at(dev, "slopes", slopes, (n_heads,), torch.float32),
         at(dev, "slots", slots, (rows,), torch.int32), n_slots, state_at,
         state_at if state_out is None else at(dev, "state_out", state_out, states, torch.float32),
-        d ** -0.5 if scale is None else scale, *rows_at(dev, "o", o, shape, dt))
+        _scale(d) if scale is None else scale, *rows_at(dev, "o", o, shape, dt))
 
 
 # acid_residual_norm_args, packed in a quarter of the time its ctypes form takes
