@@ -1273,7 +1273,7 @@ acid_status acid_linear_attention_step(int32_t dtype, int64_t n_rows, int32_t n_
     if (ld < width || ld * size % 16 || ld > ((int64_t)1 << 32))
       return set_error(ACID_ERR_SHAPE,
                        "row strides must be >= n_heads * head_dim, <= 2^32 and whole 16 bytes");
-  if (n_rows == 0) return ACID_OK;
+  if (n_rows == 0 || n_slots == 0) return ACID_OK;  // (no slots: padding rows alone)
   if (!q_dev || !k_dev || !v_dev || !slopes_dev || !state_in_dev || !state_out_dev || !o_dev)
     return set_error(ACID_ERR_INVALID_ARG, "NULL argument");
   if (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev | (uintptr_t)o_dev |

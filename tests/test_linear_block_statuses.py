@@ -7,7 +7,7 @@ import pytest
 
 import paper_2607_12358_amd as P
 from paper_2607_12358_amd import _lib as L
-from test_linear_block_args import BAD, G, SHAPE, _attend, lib  # noqa: F401  (lib: fixture)
+from test_linear_block_args import BAD, G, SHAPE, _attend, _step, lib  # noqa: F401  (lib: fixture)
 
 
 def test_a_small_workspace(lib):  # noqa: F811
@@ -55,3 +55,8 @@ def test_each_field_of_the_norms_arguments(lib, field, value, status):  # noqa: 
     assert lib.acid_residual_norm(C.byref(a), 4, 256, None) == status
     words = L.last_error()
     assert native(bytes(a), 4, 256, None) == status and L.last_error() == words
+
+
+def test_a_pool_of_no_slots_has_padding_rows_alone(lib):  # noqa: F811
+    assert _step(lib, n_slots=0, sin=None, sout=None) == 0
+    assert _step(lib, n_slots=0, sin=None, sout=None, slots=None) == SHAPE
