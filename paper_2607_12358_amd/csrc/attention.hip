@@ -73,28 +73,6 @@ __device__ __forceinline__ int swz(int r, int c) {
   else return c ^ ((r >> 1) & 7);
 }
 
-typedef __attribute__((address_space(3))) void lds_void_t;
-
-// One 16-byte-per-lane global -> LDS DMA: lane l reads 16 bytes at
-// base + off_bytes(l) and writes LDS bytes [lds + 16 l, +16).  base and lds
-// are wave-uniform (scalar registers).  Inline assembly keeps it out of the
-// compiler's wait-count bookkeeping (completion is waited for explicitly).
-__device__ __forceinline__ uint64_t uniform_ptr(const void* p) {
-  const uint64_t v = (uint64_t)(uintptr_t)p;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  return ((uint64_t)hi << 32) | lo;
-}
-__device__ __forceinline__ void dma16(uint64_t base, uint32_t off_bytes, uint32_t lds_byte) {
-  asm volatile(
-      "s_mov_b32 m0, %2\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %0, %1"
-      :
-      : "v"(off_bytes), "s"(base), "s"(lds_byte)
-      : "memory");
-}
-
 // Bijection from dispatch order to (head, query-tile) work items that gives
 // XCD x (workgroups bid = x, x+8, ...) a contiguous, head-major range, so a
 // head's K/V is streamed through as few L2s as possible.

@@ -38,6 +38,33 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+// An address that is the same in every lane, in scalar registers.
+__device__ __forceinline__ uint64_t uniform_ptr(const void* p) {
+  const uint64_t v = (uint64_t)(uintptr_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return ((uint64_t)hi << 32) | lo;
+}
+
+// One 16-byte-per-lane global -> LDS DMA: lane l reads 16 bytes at base +
+// off_bytes(l) and writes LDS bytes [lds + 16 l, +16).  base and lds are
+// wave-uniform (scalar registers).  Issued as inline assembly so the
+// compiler's wait-count pass does not see it (that pass cannot order DMA
+// completions against LDS reads and would drain every read); completion is
+// waited for explicitly.  M0 (the DMA's LDS base) is set here and nothing else
+// in the kernels that use it uses M0.
+__device__ __forceinline__ void dma16(uint64_t base, uint32_t off_bytes, uint32_t lds_byte) {
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %0, %1"
+      :
+      : "v"(off_bytes), "s"(base), "s"(lds_byte)
+      : "memory");
+}
+
 __device__ __forceinline__ float gelu_tanh(float z) {
   // 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))
   const float k0 = 0.7978845608028654f;

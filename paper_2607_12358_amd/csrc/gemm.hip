@@ -188,34 +188,11 @@ __device__ __forceinline__ void tile_coords(uint32_t t, int64_t tiles_m, int til
 
 // ------------------------------------------------------------ bf16 MFMA
 
-typedef __attribute__((address_space(3))) void lds_void_t;
-
 constexpr int BM = kGemmTile, BN = kGemmTile, BK = kGemmStep;
 constexpr int kWaves = 8;                // 2 (tokens) x 4 (features), two per SIMD
 constexpr int kTileElems = 256 * BK;     // one operand tile per stage (32 KB)
 constexpr int64_t kSplitItemFloats = 256 * 256;  // one K-split partial tile (256 KB)
 
-// One 16-byte-per-lane LDS-DMA: lane l reads 16 bytes at base + off(l) and
-// writes LDS bytes [lds + 16 l, +16).  base and lds are wave-uniform.
-// Issued as inline assembly so the compiler's wait-count pass does not see
-// it (that pass cannot order DMA completions against LDS reads and would
-// drain every read); completion is waited for explicitly.  M0 (the DMA's
-// LDS base) is set here and nothing else in these kernels uses M0.
-__device__ __forceinline__ void dma16(uint64_t base, uint32_t off_bytes, uint32_t lds_byte) {
-  asm volatile(
-      "s_mov_b32 m0, %2\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %0, %1"
-      :
-      : "v"(off_bytes), "s"(base), "s"(lds_byte)
-      : "memory");
-}
-__device__ __forceinline__ uint64_t uniform_ptr(const void* p) {
-  const uint64_t v = (uint64_t)(uintptr_t)p;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  return ((uint64_t)hi << 32) | lo;
-}
 __device__ __forceinline__ void wait_all() { __builtin_amdgcn_s_waitcnt(0); }
 
 // Epilogue of one wave's block of an output tile: 32 MB rows from mw and

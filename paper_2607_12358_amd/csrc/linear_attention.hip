@@ -287,26 +287,6 @@ __device__ __forceinline__ float decay_rate(float slope) {
   return uniform(c > 1e30f ? 1e30f : c);
 }
 
-typedef __attribute__((address_space(3))) void lds_void_t;
-
-__device__ __forceinline__ uint64_t uniform_ptr(const void* p) {
-  const uint64_t v = (uint64_t)(uintptr_t)p;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-  return ((uint64_t)hi << 32) | lo;
-}
-// Lane l copies 16 bytes at base + off_bytes(l) to LDS bytes [lds + 16 l, +16).
-// base and lds are wave-uniform; the compiler does not see the load, which
-// barrier_all() waits for.
-__device__ __forceinline__ void dma16(uint64_t base, uint32_t off_bytes, uint32_t lds_byte) {
-  asm volatile(
-      "s_mov_b32 m0, %2\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %0, %1"
-      :
-      : "v"(off_bytes), "s"(base), "s"(lds_byte)
-      : "memory");
-}
 __device__ __forceinline__ void barrier_all() {  // loads into LDS included
   __builtin_amdgcn_s_waitcnt(0);
   asm volatile("s_barrier" ::: "memory");

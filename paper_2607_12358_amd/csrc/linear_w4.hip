@@ -127,7 +127,7 @@ __device__ __forceinline__ void products(const W4Args& a) {
   // operand row col: of row `row` of the tile; past the end a copy whose result is dropped
   const int row = std::is_same_v<X, float> ? (col < 15 ? col / 3 : 4) : col;
   const int loads = R::loads(a.M < RPT ? a.M : RPT);  // of a row tile
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)red +
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_void_t*)red +
                        wave * (MT * loads * 1024);
   int rows[MT];
 #pragma unroll
