@@ -1063,16 +1063,25 @@ double alone_time(int64_t chunks, int n) {  // in chunks of outputs, of the long
 // launches they save (three bf16 chunks of outputs, half an fp32 one) and of the
 // form above.  That one / this, bf16: 16 heads of 509 tokens (d = 64) 12.6 / 10.4 us,
 // 32 of 512 (d = 128) 23.5 / 17.8, 128 of 509 (d = 64) 20.5 / 16.1, 96 of 1000 (d =
-// 128) 52.6 / 41.3, but 24 of 2045 (d = 128) 39 / 52.  Past 128 heads, with a segment each
-// in the form above, two or three: 240 of 1000 (d = 64) 44.1 / 37.0, 256 of 2000 72.3 /
-// 65.2.  Long sequences that get two workgroups a CU above keep them, but for
-// heads of 128 that get four segments there and two here (128 of 4093 190 / 170).
+// 128) 53.5 / 43.8, but 24 of 2045 (d = 128) 39 / 52; fp32: 100 of 300 (d = 64) 28.3 /
+// 21.6, 128 of 500 (d = 128) 87.7 / 74.5, but 32 of 300 (d = 128) 34.3 / 39.4.
+//
+// Past 128 heads, with a segment each in the form above, two or three, of fp32
+// (d = 64) from eight chunks on: bf16, d = 64: 150 of 500 24.1 / 19.9, 240 of 1000
+// 43.2 / 37.0, 256 of 2000 78.8 / 68.6; fp32: 150 of 500 49 / 42, 256 of 1000 96 / 92,
+// 200 of 130 21.7 / 22.4.  Heads of 128 fill a CU's LDS with two workgroups: bf16 takes
+// three segments from eight chunks on (150 of 1000 67.4 / 61.1, of 300 26.4 / 28.4),
+// two not at all while heads get one there (200 of 300 28.4 / 32.3, of 1000 68.6 / 71.7);
+// fp32 150 of 500 110 / 118, 200 of 500 112 / 140.  Long sequences that get two
+// workgroups a CU above keep them, but for heads of 128 that get four segments
+// there and two here (128 of 4093 190 / 170), or two and two (200 of 2000 152 / 141).
 int alone_of(int dtype, int64_t heads, int64_t L, int d) {
   const int64_t chunks = (L + kChunk - 1) / kChunk;
   const bool quick = dtype == ACID_BF16;
   if (chunks < 2 || heads < 1) return 0;
   if (heads > 128) {
     if (chunks < (quick ? 3 : 8) || (!quick && d == 128)) return 0;
+    if (d == 128 && heads * chunks < 512 * 8 && (chunks < 8 || 512 / heads < 3)) return 0;
     return heads <= 256 ? (int)(512 / heads) : quick && d == 64 && heads <= 384 ? 2 : 0;
   }
   const int64_t most = 256 / heads;
