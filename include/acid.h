@@ -475,8 +475,10 @@ acid_status acid_block_forward(acid_model* m, int32_t block,
  * Workspace: acid_linear_attention_workspace_needed(...) bytes (0: may be
  * NULL), 16-byte aligned, not shared by calls that may overlap; ACID_ERR_SHAPE
  * if it is smaller.  in_place: state_out is state_in; a state apart lets shorter
- * sequences do without workspace, in one launch.  ..._bytes(...) is enough for
- * both types, in place too.  Buffers 16-byte aligned, outputs apart from inputs. */
+ * sequences do without workspace, in one launch, whose sums are added in another
+ * order (the results differ by rounding).  ..._bytes(...) is enough for both types,
+ * in place too.  Buffers 16-byte aligned, outputs and workspace apart from inputs,
+ * slopes and lengths among them. */
 size_t acid_linear_attention_workspace_bytes(int64_t n_seq, int32_t n_heads,
                                              int64_t seq_len, int32_t head_dim);
 size_t acid_linear_attention_workspace_needed(int32_t dtype, int64_t n_seq, int32_t n_heads,
@@ -500,7 +502,8 @@ acid_status acid_linear_attention(int32_t dtype, int64_t n_seq, int32_t n_heads,
  * slot are one sequence's successive tokens, in row order; with slots at most
  * 65536 rows, each of which looks through the others' slots.  q, k, v, o: rows
  * of n_heads*d in `dtype`, *_ld elements apart (whole 16 bytes): columns
- * h*d .. (h+1)*d belong to head h, as in a projection's Q | K | V. */
+ * h*d .. (h+1)*d belong to head h, as in a projection's Q | K | V.  o and state_out
+ * lie apart from the inputs, slopes and slots. */
 acid_status acid_linear_attention_step(int32_t dtype, int64_t n_rows, int32_t n_heads,
                                        int32_t head_dim, const void* q_dev, int64_t q_ld,
                                        const void* k_dev, int64_t k_ld,
@@ -538,7 +541,8 @@ typedef struct {
  *   h_out = res_scale h + gate (N_post(y) post_weight)
  *   out   = (N_pre(h_out) pre_weight) (1 + scale) + shift
  * (without y, out is made from h itself).  Row r uses row r / rows_per_mod of
- * gate, shift and scale.  h, h_out and statistics fp32.  hidden % 4 == 0,
+ * gate, shift and scale.  h, h_out and statistics fp32 (sums of squares: values
+ * below 2^56).  hidden % 4 == 0,
  * <= 8192; rows <= 2^23; row strides in elements, multiples of 4; matrices
  * aligned to four of their elements, vectors to 16 bytes; outputs apart from
  * everything but h_out from h (columns of one matrix may interleave). */
@@ -561,7 +565,8 @@ acid_status acid_quantize_w4(const float* w_dev, int32_t N, int32_t K, int32_t g
 /* out = act(x w^T + bias) for few rows (meant for up to 64; at most 65536): x
  * [M][x_ld] in x_dtype, whole 16 bytes apart; out [M][out_ld] in out_dtype;
  * bias fp32 [N] or NULL; kind ACID_EPI_BIAS or ACID_EPI_BIAS_GELU.  fp32 rows
- * are not rounded; accumulation fp32.  |x| < 2^120. */
+ * are not rounded; accumulation fp32.  |x| < 2^120: past it, infinities included,
+ * that row's outputs may be NaN. */
 acid_status acid_linear_w4(int32_t x_dtype, int64_t M, int32_t N, int32_t K, int32_t group,
                            const void* x_dev, int64_t x_ld, const void* codes_dev,
                            const float* scales_dev, const float* bias_dev, int32_t kind,
