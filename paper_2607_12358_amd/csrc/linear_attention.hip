@@ -193,13 +193,14 @@ hipError_t launch_step(int dtype, int d, const StepArgs& a, hipStream_t s) {
 // K's operand of the outer products lies across those rows; bf16 reads it with
 // the transposing LDS load.
 //
-// 12 heads of 32760 tokens (d = 128, bf16) take 162 us in three launches: the
-// segments' states 51 us (239 MB), the scan of them 12 (62 MB) and the outputs 95
-// (480 MB), 4.7 to 5.2 TB/s where a copy makes 5.0.  K and V are read twice,
+// 12 heads of 32760 tokens (d = 128, bf16) take 163 us in three launches: the
+// segments' states 51 us (239 MB), the scan of them 11 (62 MB) and the outputs 96
+// (480 MB) at best, 4.7 to 5.4 TB/s where a copy makes 5.0 (medians of traced launches
+// over two sets of inputs 57, 14 and 125).  K and V are read twice,
 // because a segment's outputs need the states of those before it, and V's lines
 // that two chunks share come from beyond L2 again for the second now and then
-// (45 MB; the last reads of Q and K marked as such halve that, but 1 x 30000 with d
-// = 64 then takes 88 us for 85).  With all reads from L2 the outputs took 94 us for 97:
+// (45 MB; the last reads of Q and K marked as such halve that, for no time here and
+// 3% more with d = 64).  With all reads from L2 the outputs took 94 us for 97:
 // the vector units issue for half of that time (S and the scores made into
 // operands, V decayed), with 16 waves a CU to hide the rest: 80 KB of LDS and 128
 // registers a lane are what two workgroups have.  One wave for 32 columns, half as
@@ -1021,15 +1022,15 @@ __global__ __launch_bounds__(4 * D, sizeof(T) == 2 ? 4 : 2) void la_chunk_kernel
 // Tokens of a segment, a multiple of 64, and how many there are: as many as
 // give each CU a workgroup, or two where they then have eight chunks each (one
 // segment a head once the heads alone do).  With 256 / 512 workgroups: 12 x 4680
-// tokens (d = 128) 42 / 48 us, 1 x 30000 42 / 61, 4 x 8192 (d = 64) 23 / 29, but 12
-// x 32760 167 / 157 and 24 x 32760 318 / 301.
+// tokens (d = 128) 42 / 50 us, but 12 x 32760 163 / 158, with d = 64 85 / 71, and 24 x
+// 32760 313 / 306.
 //
 // A bf16 chunk takes about as long as its segment's state costs to write, sum and
 // read, so segments have two unless there are few of them (one chunk / two,
-// d = 128: 32 x 512 tokens 33 / 24 us, 16 x 640 24 / 22, but 8 x 1024 23.3 / 24.6, and
-// with d = 64 4 x 1559 13.5 / 15.1), and up to four stay together (64 x 256: 25 in
-// four segments, 21 in two, 19 in one).  An fp32 chunk takes three times as long
-// (8 x 2000: one 44 us, two 54).
+// d = 128: 32 x 512 tokens 33 / 26 us, 16 x 640 24.7 / 22.6, but 8 x 1024 24.6 / 25.3,
+// and with d = 64 4 x 1559 13.0 / 15.1), and up to four stay together (64 x 256: 26 in
+// four segments, 23 in two, 20 in one).  An fp32 chunk takes three times as long
+// (8 x 2000, d = 128: one 44 us, two 54).
 struct Segments {
   int64_t tokens, count;
 };
@@ -1045,9 +1046,11 @@ Segments segments_of(int dtype, int64_t heads, int64_t L) {
 }
 
 // Up to this many segments the outputs' kernel adds those before its own
-// itself; more take a scan, a launch of its own (folded / scanned, d = 128: 6
-// segments of 24 x 1500 tokens 35.9 / 36.8 us, 8 of 32 x 2000 47.1 / 44.9; d = 64: 8 of
-// 32 x 2000 24.3 / 26.0, 25 of 4 x 1559 16.8 / 12.8).
+// itself; more take a scan, a launch of its own (folded / scanned, d = 128: 5
+// segments of 48 x 1280 tokens 40.1 / 41.4 us, 6 of 40 x 1536 41.7 / 41.8, 8 of 32 x
+// 2000 47.8 / 45.8; d = 64: 8 of 32 x 2000 25.1 / 26.2, 9 of 28 x 1728 22.7 / 21.9, 25
+// of 4 x 1559 15.8 / 13.1; fp32, d = 64: 5 of 8 x 300 14.0 / 15.8, 10 of 8 x 600 16.7 /
+// 15.8; d = 128: 7 of 8 x 400 30.4 / 30.3, 8 of 8 x 500 34.4 / 32.5).
 int64_t most_folded(int d) { return d == 64 ? 8 : 6; }
 
 // Segments that each make the state before them from the sequence's start: one

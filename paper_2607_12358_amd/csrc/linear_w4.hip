@@ -4,7 +4,7 @@
 //   out[m][n] = act(sum_k x[m][k] (c[n][k] - 8) s[n][k / group] + bias[n])
 //
 // Bound by reading the codes once (HBM: 28672 x 8192 with groups of 128, 125 MB, 8
-// bf16 rows, 25 us, 5.0 TB/s), so the layout is the one the matrix
+// bf16 rows, 26 us, 4.8 TB/s), so the layout is the one the matrix
 // instruction takes: a tile is 16 outputs x 128 inputs, 1 KB, and lane l of
 // the wave that reads it gets the 16 bytes of output l % 16 whose word j
 // holds inputs 32 j + 8 (l / 16) .. + 7, its share of the j-th 16x16x32
@@ -102,8 +102,8 @@ struct W4Args {
   int32_t M, N, K, gelu;
 };
 
-// Sixteen waves pay where few tiles meet many blocks: 1536 x 8960, one row, 8 / 16
-// waves 7.0 / 6.3 us (4608 x 1536, 8 / 12 waves: 4.0 / 4.3).
+// Sixteen waves pay where few tiles meet many blocks: 1536 x 8960, 8 / 16 waves, one
+// row 7.2 / 5.9 us, four 7.1 / 6.3 (4608 x 1536, 8 / 12 waves: 3.8 / 4.2).
 template <int NT, int MT>
 constexpr int MOST_WAVES = NT * MT == 1 ? 16 : 8;
 
@@ -320,7 +320,8 @@ hipError_t launch_group(int group, const W4Args& a, hipStream_t s) {
 
 // One thread per output and group: scale = max |w| / 7 (NaN if a weight of
 // the group is not finite), code = w / scale rounded to nearest, ties to
-// even, + 8.  Outputs past N, up to a whole tile, get scale 0 and code 8.
+// even, + 8.  Outputs past N, up to a whole tile, get scale 0 and code 8.  Reads w
+// twice: 28672 x 8192 takes 408 us, where a copy of its 1.06 GB takes 214.
 template <int GROUP>
 __global__ __launch_bounds__(256) void quantize_w4_kernel(const float* __restrict__ w, int N,
                                                           int K, uint8_t* __restrict__ codes,

@@ -6,7 +6,9 @@
 // N is LayerNorm (biased variance), RMS norm or nothing.  HBM-bound: y and h
 // are read once, h' and out written once; a row stays in registers, in fp32,
 // between its two norms.  32760 rows of 1536 (y and out bf16), 604 MB: 115 us, 5.2
-// TB/s, where a copy makes 5.0; 4 rows of 4096: 4.0 us.
+// TB/s, where a 1 GiB copy makes 5.0 (with a modulation row for each, 1208 MB: 232);
+// 4 rows of 4096: 4.0 us.  Short rows leave lanes of their one wave idle: 100000 of
+// 64, 77 MB: 33 us.
 #include <math.h>
 
 #include <type_traits>
@@ -226,9 +228,10 @@ template <typename Y, typename Out>
 hipError_t launch(const NormArgs& a, hipStream_t s) {
   const int n4 = a.hidden / 4;
   // Runs of up to four rows, of fewer where four would leave less than 1024
-  // waves.  32760 rows of 1536 with 1 / 2 / 3 / 4 / 6 / 8 rows each: 145 / 125 /
-  // 119 / 119 / 122 / 125 us; 8000 of 4096: 137 / 100 / 95 / 87 / 89 / 86; 1000 of
-  // 1024 (fp32, 2 / 3 / 4 / 8): 9.9 / 9.7 / 10.5 / 13.1.
+  // waves.  32760 rows of 1536 with 1 / 2 / 3 / 4 / 6 / 8 rows each: 122 / 113 /
+  // 114 / 116 / 120 / 122 us; 8000 of 4096: 76 / 74 / 78 / 78 / 84 / 81; 4000 of 8192:
+  // 99 / 84 / 85 / 79 / 82 / 80; 100000 of 64: 42 / 35 / 33 / 33 / 34 / 35; 1000 of 1024
+  // (fp32): 5.5 / 6.7 / 7.9 / 8.6 / 11.0 / 13.3.
 #define RN(W, C)                                                                               \
   do {                                                                                         \
     const int64_t most = a.rows / (1024 / W);                                                  \
