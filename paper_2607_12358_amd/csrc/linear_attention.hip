@@ -857,7 +857,8 @@ __device__ __forceinline__ void chunks_of(const ChunkArgs& a, unsigned char* row
   }
   // (made while the loads above are on their way)  Over a chunk, and over the ragged
   // one at a sequence's end; for a state that is only read by a segment's own bf16
-  // outputs one part will do.
+  // outputs one part will do (2^-25 a chunk; what 288 GB hold gives a segment at most
+  // 8600 of them, 2^-12 where a bf16 value is rounded by 2^-8).
   constexpr bool TWO_PART_DECAY = LAST || sizeof(T) == 4;
   const Decay whole(slope, kChunk), ragged(slope, (int)(end - begin) & (kChunk - 1));
   float tile_decay[4];
