@@ -573,6 +573,111 @@ acid_status acid_linear_w4(int32_t x_dtype, int64_t M, int32_t N, int32_t K, int
                            int32_t out_dtype, void* out_dev, int64_t out_ld,
                            hipStream_t stream);
 
+/* ------------------- the 8-bit block: e4m3 products, heads with positions */
+
+/* e4m3 rows: codes [rows][K] of one byte (OCP e4m3: finite, up to 448), and for each
+ * row and group of 128 inputs (the last may be shorter) an fp32 scale, value = code
+ * scale; scales are laid out [ceil(K/128)][scales_ld], scales_ld >= round_up(rows, 4)
+ * and a multiple of 4 (entries past `rows` are neither written nor used).
+ *   scale = max(max |x| / 448, 2^-126), code = x (1 / scale) to nearest, ties to even
+ * A group with an infinity or a NaN gets scale NaN and codes that mean nothing.  K is a
+ * multiple of 16, <= 2^22, ceil(rows / 32) ceil(K / 128) <= 2^26; matrices' rows lie
+ * whole 16 bytes apart, buffers are 16-byte aligned and apart from one another.
+ *
+ * acid_quantize_fp8: rows x [rows][x_ld] in x_dtype. */
+acid_status acid_quantize_fp8(int32_t x_dtype, int64_t rows, int32_t K, const void* x_dev,
+                              int64_t x_ld, void* codes_dev, int64_t codes_ld, float* scales_dev,
+                              int64_t scales_ld, hipStream_t stream);
+
+/* LN(x) (1 + scale) + shift per row (acid_ln_modulate's function) straight into e4m3
+ * rows.  x fp32 [rows][x_ld]; row r uses row r / rows_per_mod of shift_dev and
+ * scale_dev, fp32 [n_mod][hidden] (0: one row for all).  hidden <= 8192, rows <= 2^23. */
+acid_status acid_ln_modulate_fp8(int64_t rows, int32_t hidden, const float* x_dev, int64_t x_ld,
+                                 const float* shift_dev, const float* scale_dev,
+                                 int64_t rows_per_mod, void* codes_dev, int64_t codes_ld,
+                                 float* scales_dev, int64_t scales_ld, hipStream_t stream);
+
+/* e4m3 weights: codes [N][K], fp32 scales [ceil(N/128)][ceil(K/128)], one for each block
+ * of 128 outputs and 128 inputs, made as those of rows, from fp32 w [K][N] ([in][out],
+ * as the manifest has it).  K a multiple of 16, K and N <= 2^22. */
+acid_status acid_quantize_fp8_weight(const float* w_dev, int32_t N, int32_t K, void* codes_dev,
+                                     float* scales_dev, hipStream_t stream);
+
+typedef struct {
+  const void* a;             /* e4m3 rows [M][a_ld] */
+  int64_t a_ld;
+  const float* a_scales;     /* [ceil(K/128)][a_scales_ld] */
+  int64_t a_scales_ld;
+  const void* w;             /* e4m3 weights [N][K] */
+  const float* w_scales;     /* [ceil(N/128)][ceil(K/128)] */
+  const float* bias;         /* [N], NULL: 0 */
+  const float* gate;         /* [N], GATE_RESIDUAL only */
+  const float* residual;     /* fp32 [M][residual_ld], GATE_RESIDUAL only; may be out itself */
+  int64_t residual_ld;
+  void* out;                 /* [M][out_ld] in out_dtype */
+  int64_t out_ld;
+  void* workspace;           /* 16-byte aligned; not shared by calls that may overlap */
+  size_t workspace_bytes;
+  int32_t kind;              /* acid_epilogue: BIAS, BIAS_GELU or GATE_RESIDUAL */
+  int32_t out_dtype;         /* GATE_RESIDUAL: ACID_F32 */
+} acid_linear_fp8_args;
+
+/* y = a w^T + bias with the rows' and the weights' scales, accumulated in fp32;
+ * out = y (BIAS), GELU_tanh(y) (BIAS_GELU), residual + gate (.) y (GATE_RESIDUAL).  Any M
+ * from a single row on (<= 2^24) and any N; K a multiple of 16, K and N <= 2^22; a_ld <
+ * 2^24.  Plain and GELU outputs in fp32 come from exact products and fp32 sums; bf16 ones
+ * and the gated y from the 8-bit matrix units, whose sums are about 1.4e-5 off.  out
+ * lies apart from everything but the residual.  Workspace:
+ * acid_linear_fp8_workspace_needed(...) bytes (0: may be NULL), ACID_ERR_SHAPE if
+ * it is smaller.  A NaN code or scale makes NaN the outputs it belongs to, no others. */
+size_t acid_linear_fp8_workspace_needed(int64_t M, int32_t N, int32_t K);
+acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t N, int32_t K,
+                            hipStream_t stream);
+
+/* Norm of Q's and K's heads before their rotation: LAYER and RMS over each head (as
+ * acid_norm_kind), RMS_ROW over all heads of a token. */
+typedef enum {
+  ACID_HEAD_NORM_NONE = 0,
+  ACID_HEAD_NORM_LAYER = 1,
+  ACID_HEAD_NORM_RMS = 2,
+  ACID_HEAD_NORM_RMS_ROW = 3
+} acid_head_norm;
+
+typedef struct {
+  const void *q, *k, *v;     /* rows [n_seq * tokens][*_ld] in in_dtype, NULL: none */
+  int64_t q_ld, k_ld, v_ld;
+  void *q_out, *k_out, *vt;  /* in out_dtype, each with its input */
+  int64_t q_head, q_row, q_seq;    /* strides in elements of q_out's heads, tokens and */
+  int64_t k_head, k_row, k_seq;    /* sequences; vt's row is one dim, its tokens lie */
+  int64_t vt_head, vt_row, vt_seq; /* side by side */
+  const void* positions;     /* [axes][positions_ld], int32 or fp32, one a token */
+  int64_t positions_ld;
+  const double* freqs;       /* [pairs], radians for one step along the pair's axis */
+  const float *q_weight, *k_weight; /* [head_dim]; RMS_ROW: [heads * head_dim]; NULL: 1 */
+  const float *q_bias, *k_bias;     /* [head_dim], LAYER only; NULL: 0 */
+  int32_t in_dtype, out_dtype;
+  int32_t heads, kv_heads, head_dim;
+  int32_t axes, sections[4]; /* pairs that turn by each axis, in their order */
+  int32_t pairing;           /* 0: pair i is dims 2 i and 2 i + 1; 1: i and i + pairs */
+  int32_t norm;              /* acid_head_norm */
+  int32_t positions_f32;     /* 1: positions are fp32 */
+  float q_scale, eps;
+} acid_rotary_qkv_args;
+
+/* A projection's rows into attention's heads: Q and K normed (norm, weight, bias), each
+ * pair (x, y) turned by the angle t = position freq to (x cos t - y sin t, x sin t + y
+ * cos t), dims past the pairs left as they are; Q times q_scale (acid_q_scale(d) for
+ * attention's q_prescaled, or 1); V transposed.  Angles are taken in 64 bits, the
+ * rest in fp32, rounded once.  Position 0 on every axis turns by nothing (text).
+ * head_dim 64 or 128; pairs <= head_dim / 2 in all, in pairing 1 a multiple of 8.
+ * Contiguous q_out [n_seq][heads][tokens][d] is attention's; other strides write
+ * into a cache's rows or keep tokens outermost.  q, k, v, q_out, k_out, weights and
+ * biases 16-byte aligned, rows and strides of the first five whole 16 bytes; vt as its
+ * elements.  Outputs apart from all else, but q_out may be q's own rows (of its type,
+ * tokens outermost), k_out k's. */
+acid_status acid_rotary_qkv(const acid_rotary_qkv_args* args, int64_t n_seq, int64_t tokens,
+                            hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,13 +18,16 @@ from ._lib import (ACID_BF16, ACID_CACHE_APPLY, ACID_CACHE_STORE, ACID_EPI_BIAS,
                    ACID_EPI_BIAS_GELU, ACID_EPI_EULER, ACID_EPI_GATE_RESIDUAL, ACID_EPI_QKV,
                    ACID_EPI_QKV_GELU, ACID_BLOCK_PARALLEL, ACID_BLOCK_SEQUENTIAL,
                    ACID_F32, ACID_MODE_ACID, ACID_MODE_DICACHE, ACID_MODE_EASYCACHE,
-                   ACID_MODE_NOCACHE, ACID_NORM_LAYER, ACID_NORM_NONE, ACID_NORM_RMS,
+                   ACID_HEAD_NORM_LAYER, ACID_HEAD_NORM_NONE, ACID_HEAD_NORM_RMS,
+                   ACID_HEAD_NORM_RMS_ROW, ACID_MODE_NOCACHE, ACID_NORM_LAYER, ACID_NORM_NONE, ACID_NORM_RMS,
                    KERNEL_CLASSES, AcidError,
                    TRACE_DTYPE, check, lib)
 
 __all__ = ["Model", "gate", "GateState", "gate_device_sequence", "cache_apply", "easycache_reuse", "attention", "linear",
            "ln_modulate", "linear_attention", "linear_attention_step", "linear_attention_workspace",
-           "linear_w4", "quantize_w4", "w4_shapes", "residual_norm", "q_scale", "version", "AcidError", "KERNEL_CLASSES"]
+           "linear_w4", "quantize_w4", "w4_shapes", "residual_norm",
+           "linear_fp8", "linear_fp8_workspace", "quantize_fp8", "quantize_fp8_weight", "fp8_shapes", "fp8_weight_shapes",
+           "ln_modulate_fp8", "rotary_qkv", "q_scale", "version", "AcidError", "KERNEL_CLASSES"]
 
 
 def _torch():
@@ -171,11 +174,11 @@ def linear(a, wt, kind: int, bias, gate=None, out=None, v_out=None, q=None, k=No
     check(lib().acid_linear(code, M, N, K, _ptr(a), _ptr(wt), C.byref(e), _stream(stream)))
 
 
-# ------------------------------------------------ linear-attention block
+# ---------------------------- linear-attention block, and the 8-bit block
 #
 # A call for a few tokens is bound by the host, so tensors are looked at by the
-# native module _binding, which calls _at and _rows_at below for those that are
-# not as they have to be, and calls the library.
+# native module _binding, which calls _at, _rows_at and _heads_at below for those
+# that are not as they have to be, and calls the library.
 
 
 def _dtype_code(torch, t, name: str) -> int:
@@ -223,6 +226,20 @@ def _rows_at(dev, name: str, t, shape: tuple, dtype):
     raise ValueError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)}")
 
 
+def _heads_at(dev, name: str, t, shape: tuple, dtype):
+    """(address, head stride, row stride, sequence stride) of a [heads, rows, width] or
+    [n_seq, heads, rows, width] tensor on GPU dev of this shape and type, of unit last
+    stride; the last is 0 where there is one sequence."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev:
+        strides = t.stride()
+        if len(shape) in (3, 4) and (strides[-1] == 1 or shape[-1] == 1):
+            return t.data_ptr(), strides[-3], strides[-2], strides[0] if len(shape) == 4 and shape[0] > 1 else 0
+        raise ValueError(f"{name}: expected heads of unit last stride, got strides {strides}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: expected a tensor on GPU {dev}, got one on {t.device}")
+    raise ValueError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} {tuple(t.shape)}")
+
+
 _bound = None
 
 
@@ -236,8 +253,9 @@ def _native():
         except ImportError as e:
             raise RuntimeError("_binding.so is missing: build it with "
                                "`python -m paper_2607_12358_amd.build`") from e
-        N.bind(getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), torch.Tensor, _at, _rows_at,
-               ((torch.bfloat16, 4, 16), (torch.float32, 2, 32), (torch.int32, 0, 32), (torch.uint8, 1, 8)),
+        N.bind(getattr(torch.Tensor, "__dlpack_c_exchange_api__", None), torch.Tensor, _at, _rows_at, _heads_at,
+               ((torch.bfloat16, 4, 16), (torch.float32, 2, 32), (torch.int32, 0, 32), (torch.uint8, 1, 8),
+                (torch.float8_e4m3fn, 10, 8), (torch.float64, 2, 64)),
                {name: C.cast(getattr(lib(), name), C.c_void_p).value for name in _L._SIGS})
         _bound = torch, N, N.at, N.rows_at
     return _bound
@@ -426,6 +444,198 @@ def linear_w4(x, codes, scales, out, bias=None, gelu: bool = False, stream=None)
         at(dev, "bias", bias, (n,), torch.float32),
         ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS, _dtype_code(torch, out, "out"),
         *rows_at(dev, "out", out, (m, n), out.dtype))
+
+
+def fp8_shapes(rows: int, k: int):
+    """Shapes of the codes (torch.float8_e4m3fn) and scales (fp32) of [rows, k]
+    e4m3 rows: value [r, i] is codes[r, i] * scales[i // 128, r]."""
+    if rows < 0 or k < 16 or k % 16:
+        raise ValueError("rows >= 0, k a multiple of 16")
+    return (rows, k), (-(-k // 128), (rows + 3) // 4 * 4)
+
+
+def fp8_weight_shapes(n: int, k: int):
+    """Shapes of the codes (torch.float8_e4m3fn) and scales (fp32) of an [n outputs, k
+    inputs] e4m3 weight: value [o, i] is codes[o, i] * scales[o // 128, i // 128]."""
+    if n < 1 or k < 16 or k % 16:
+        raise ValueError("n >= 1, k a multiple of 16")
+    return (n, k), (-(-n // 128), -(-k // 128))
+
+
+def _fp8_at(torch, rows_at, dev, codes, scales, rows: int, k: int, names=("codes", "scales")):
+    """Codes' address and row stride, scales' address and row stride, of e4m3 rows."""
+    blocks, padded = -(-k // 128), (rows + 3) // 4 * 4
+    return (*rows_at(dev, names[0], codes, (rows, k), torch.float8_e4m3fn),
+            *rows_at(dev, names[1], scales, (blocks, padded), torch.float32))
+
+
+def quantize_fp8(x, codes, scales, stream=None) -> None:
+    """e4m3 codes and scales (fp8_shapes) of the rows x [rows, k], bf16 or fp32: for each
+    row and 128 inputs scale = max |x| / 448, code = x / scale.  x, codes and scales may
+    be row-strided."""
+    torch, N, at, rows_at = _native()
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows, k]")
+    rows, k = x.shape
+    dev = _device(x, "x")
+    _on(torch, dev, stream, N.quantize_fp8, _dtype_code(torch, x, "x"), rows, k,
+        *rows_at(dev, "x", x, (rows, k), x.dtype), *_fp8_at(torch, rows_at, dev, codes, scales, rows, k))
+
+
+def quantize_fp8_weight(w, codes, scales, stream=None) -> None:
+    """e4m3 codes and scales (fp8_weight_shapes) of the fp32 weight w [k inputs, n
+    outputs], a scale for each 128 x 128 block."""
+    torch, N, at, rows_at = _native()
+    if w.dim() != 2:
+        raise ValueError("w: expected [k, n]")
+    k, n = w.shape
+    dev = _device(w, "w")
+    _on(torch, dev, stream, N.quantize_fp8_weight, at(dev, "w", w, (k, n), torch.float32), n, k,
+        at(dev, "codes", codes, (n, k), torch.float8_e4m3fn),
+        at(dev, "scales", scales, (-(-n // 128), -(-k // 128)), torch.float32))
+
+
+def ln_modulate_fp8(x, shift, scale, codes, scales, rows_per_mod: int = 0, stream=None) -> None:
+    """ln_modulate, LN(x) (1 + scale) + shift, of the fp32 rows x [rows, hidden] into e4m3
+    codes and scales (fp8_shapes).  shift, scale fp32 [hidden], or [n_mod, hidden] with
+    row r using row r // rows_per_mod.  x, codes and scales may be row-strided."""
+    torch, N, at, rows_at = _native()
+    f32 = torch.float32
+    if x.dim() != 2:
+        raise ValueError("x: expected [rows, hidden]")
+    if rows_per_mod < 0:
+        raise ValueError("rows_per_mod < 0")
+    rows, hidden = x.shape
+    dev, n_mod = _device(x, "x"), -(-rows // rows_per_mod) if rows_per_mod else 1
+
+    def vector(name, t):
+        return at(dev, name, t, (hidden,) if n_mod == 1 and t.dim() == 1 else (n_mod, hidden), f32)
+
+    _on(torch, dev, stream, N.ln_modulate_fp8, rows, hidden, *rows_at(dev, "x", x, (rows, hidden), f32),
+        vector("shift", shift), vector("scale", scale), rows_per_mod,
+        *_fp8_at(torch, rows_at, dev, codes, scales, rows, hidden))
+
+
+def linear_fp8_workspace(m: int, n: int, k: int) -> int:
+    """Bytes of workspace that linear_fp8 of these sizes takes."""
+    return int(lib().acid_linear_fp8_workspace_needed(m, n, k))
+
+
+_FP8_ARGS = struct.Struct("@PqPqPPPPPqPqPNii")  # acid_linear_fp8_args
+
+
+def linear_fp8(a, a_scales, w, w_scales, out, bias=None, gelu: bool = False, gate=None, residual=None,
+               workspace=None, stream=None) -> None:
+    """y = a w^T + bias of e4m3 rows a [m, k] (quantize_fp8, ln_modulate_fp8) and e4m3
+    weights w [n, k] (quantize_fp8_weight); out [m, n], bf16 or fp32, is y, GELU(y) with
+    gelu, or with gate (fp32 [n]) and residual (fp32 [m, n], out itself will do)
+    residual + gate y in fp32.  bias fp32 [n].  a, a_scales, residual and out may be
+    row-strided.  workspace: uint8 tensor of linear_fp8_workspace bytes, kept by callers
+    whose calls must not allocate; by default one is taken from torch's allocator."""
+    torch, N, at, rows_at = _native()
+    f32 = torch.float32
+    if a.dim() != 2 or out.dim() != 2:
+        raise ValueError("a and out: expected two axes")
+    if (gate is None) != (residual is None) or (gate is not None and gelu):
+        raise ValueError("gate and residual go together, without gelu")
+    (m, k), n = a.shape, out.shape[1]
+    dev = _device(a, "a")
+    if workspace is None:
+        size = N.linear_fp8_workspace_needed(m, n, k)
+        if size:
+            with torch.cuda.stream(stream):  # its memory goes back to that stream's pool
+                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+    else:
+        size = workspace.numel()
+    args = _FP8_ARGS.pack(
+        *_fp8_at(torch, rows_at, dev, a, a_scales, m, k, ("a", "a_scales")),
+        at(dev, "w", w, (n, k), torch.float8_e4m3fn),
+        at(dev, "w_scales", w_scales, (-(-n // 128), -(-k // 128)), f32),
+        at(dev, "bias", bias, (n,), f32) or 0, at(dev, "gate", gate, (n,), f32) or 0,
+        *((0, 0) if residual is None else rows_at(dev, "residual", residual, (m, n), f32)),
+        *rows_at(dev, "out", out, (m, n), out.dtype),
+        0 if workspace is None else at(dev, "workspace", workspace, (size,), torch.uint8), size,
+        ACID_EPI_GATE_RESIDUAL if gate is not None else ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS,
+        _dtype_code(torch, out, "out"))
+    _on(torch, dev, stream, N.linear_fp8, args, m, n, k)
+
+
+_ROTARY_ARGS = struct.Struct("@PPPqqqPPPqqqqqqqqqPqPPPPPiiiiiiiiiiiiiff4x")  # acid_rotary_qkv_args
+_HEAD_NORMS = {"none": ACID_HEAD_NORM_NONE, "layer": ACID_HEAD_NORM_LAYER, "rms": ACID_HEAD_NORM_RMS,
+               "rms_row": ACID_HEAD_NORM_RMS_ROW}
+_PAIRINGS = {"adjacent": 0, "halves": 1}
+
+
+def rotary_qkv(q, k, v, positions, freqs, sections: Sequence[int], q_out, k_out, vt, pairs: str = "adjacent",
+               norm: str = "none", q_weight=None, k_weight=None, q_bias=None, k_bias=None,
+               q_scale: float = 1.0, eps: float = 1e-6, stream=None) -> None:
+    """A projection's rows into attention's heads: Q and K normed and rotated, Q times
+    q_scale (the function of that name gives the one that attention's q_prescaled
+    takes), V transposed.
+    q [rows, heads*d], k, v [rows, kv_heads*d], bf16 or fp32, unit column stride (columns
+    of one projection's output will do), rows = tokens, or n_seq * tokens; q_out [heads,
+    tokens, d], k_out [kv_heads, tokens, d], vt [kv_heads, d, tokens], with an n_seq
+    axis before them for several sequences, all bf16 or all fp32, unit last stride (rows
+    of a longer cache will do).  Any of q, k, v may be None with its output.
+    positions [axes, rows], int32 or fp32 (one axis: [rows] too); freqs fp64 [pairs],
+    radians a step; sections: how many of the pairs turn by each axis.  Pairs are
+    "adjacent" dims (2i, 2i+1) or "halves" (i, i + pairs); dims past them do not turn.
+    norm "none", "layer" or "rms" over each head, or "rms_row" over a token's heads;
+    weights fp32 [d] ("rms_row": [heads*d]), biases fp32 [d] with "layer"."""
+    torch, N, at, rows_at = _native()
+    f32 = torch.float32
+    if norm not in _HEAD_NORMS:
+        raise ValueError(f"unknown norm {norm!r}")
+    if pairs not in _PAIRINGS:
+        raise ValueError(f"unknown pairs {pairs!r}")
+    if not 1 <= len(sections) <= 4:
+        raise ValueError("sections: one to four axes")
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (vt is None):
+        raise ValueError("q and q_out, k and k_out, v and vt go together")
+    some, out = next(((i, o) for i, o in ((q, q_out), (k, k_out), (v, vt)) if i is not None), (None, None))
+    if some is None:
+        raise ValueError("none of q, k and v")
+    if some.dim() != 2 or out.dim() not in (3, 4):
+        raise ValueError("expected rows [rows, heads*d] and heads [heads, tokens, d] or [n_seq, heads, tokens, d]")
+    dev, rows, dt, odt = _device(some, "q, k and v"), some.shape[0], some.dtype, out.dtype
+    lead = tuple(out.shape[:-3])
+    n_seq = lead[0] if lead else 1
+    tokens, d = (out.shape[-1], out.shape[-2]) if out is vt else (out.shape[-2], out.shape[-1])
+    if n_seq * tokens != rows:
+        raise ValueError(f"{rows} rows for {n_seq} sequences of {tokens} tokens")
+    heads = q_out.shape[-3] if q is not None else 0
+    kv_out = k_out if k is not None else vt
+    kv_heads = kv_out.shape[-3] if kv_out is not None else 0
+    nothing, no_heads = (0, 0), (0, 0, 0, 0)
+    q_at, q_ld = nothing if q is None else rows_at(dev, "q", q, (rows, heads * d), dt)
+    k_at, k_ld = nothing if k is None else rows_at(dev, "k", k, (rows, kv_heads * d), dt)
+    v_at, v_ld = nothing if v is None else rows_at(dev, "v", v, (rows, kv_heads * d), dt)
+    N_heads = N.heads_at
+    qo = no_heads if q is None else N_heads(dev, "q_out", q_out, lead + (heads, tokens, d), odt)
+    ko = no_heads if k is None else N_heads(dev, "k_out", k_out, lead + (kv_heads, tokens, d), odt)
+    vo = no_heads if v is None else N_heads(dev, "vt", vt, lead + (kv_heads, d, tokens), odt)
+    axes, n_pairs = len(sections), sum(sections)
+    where = pos_ld = turns = 0
+    if n_pairs and (q is not None or k is not None):
+        pdt = positions.dtype
+        if pdt is not torch.int32 and pdt is not f32:
+            raise ValueError(f"positions: expected int32 or float32, got {pdt}")
+        if axes == 1 and positions.dim() == 1:
+            where, pos_ld = at(dev, "positions", positions, (rows,), pdt), rows
+        else:
+            where, pos_ld = rows_at(dev, "positions", positions, (axes, rows), pdt)
+            pos_ld = max(pos_ld, rows)
+        turns = at(dev, "freqs", freqs, (n_pairs,), torch.float64)
+    each = norm == "rms_row"
+    a = _ROTARY_ARGS.pack(
+        q_at, k_at, v_at, q_ld, k_ld, v_ld, qo[0], ko[0], vo[0], *qo[1:], *ko[1:], *vo[1:], where, pos_ld, turns,
+        at(dev, "q_weight", q_weight, (heads * d if each else d,), f32) or 0,
+        at(dev, "k_weight", k_weight, (kv_heads * d if each else d,), f32) or 0,
+        at(dev, "q_bias", q_bias, (d,), f32) or 0, at(dev, "k_bias", k_bias, (d,), f32) or 0,
+        _dtype_code(torch, some, "q, k and v"), _dtype_code(torch, out, "q_out, k_out and vt"),
+        heads, kv_heads, d, axes, *sections, *(0,) * (4 - axes), _PAIRINGS[pairs], _HEAD_NORMS[norm],
+        int(where != 0 and pdt is f32), q_scale, eps)
+    _on(torch, dev, stream, N.rotary_qkv, a, n_seq, tokens)
 
 
 # ------------------------------------------------------------------ model

@@ -25,6 +25,8 @@ ACID_CACHE_STORE, ACID_CACHE_APPLY = 0, 1
  ACID_EPI_EULER, ACID_EPI_QKV_GELU) = range(6)
 ACID_BLOCK_SEQUENTIAL, ACID_BLOCK_PARALLEL = 0, 1
 ACID_NORM_NONE, ACID_NORM_LAYER, ACID_NORM_RMS = 0, 1, 2
+(ACID_HEAD_NORM_NONE, ACID_HEAD_NORM_LAYER, ACID_HEAD_NORM_RMS,
+ ACID_HEAD_NORM_RMS_ROW) = range(4)
 KERNEL_CLASSES = ("temb", "ln_mod", "gemm_qkv", "attention", "gemm_proj", "gemm_ffn1",
                   "gemm_ffn2", "gemm_head", "drift", "cache", "misc")
 
@@ -75,6 +77,29 @@ class ResidualNormArgsC(C.Structure):
                 ("post_weight", C.c_void_p), ("pre_weight", C.c_void_p), ("gate", C.c_void_p),
                 ("shift", C.c_void_p), ("scale", C.c_void_p), ("rows_per_mod", C.c_int64),
                 ("res_scale", C.c_float), ("eps", C.c_float)]
+
+
+class LinearFp8ArgsC(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("a_ld", C.c_int64), ("a_scales", C.c_void_p),
+                ("a_scales_ld", C.c_int64), ("w", C.c_void_p), ("w_scales", C.c_void_p),
+                ("bias", C.c_void_p), ("gate", C.c_void_p), ("residual", C.c_void_p),
+                ("residual_ld", C.c_int64), ("out", C.c_void_p), ("out_ld", C.c_int64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("kind", C.c_int32), ("out_dtype", C.c_int32)]
+
+
+class RotaryQkvArgsC(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "v")]
+                + [(n, C.c_int64) for n in ("q_ld", "k_ld", "v_ld")]
+                + [(n, C.c_void_p) for n in ("q_out", "k_out", "vt")]
+                + [(f"{t}_{n}", C.c_int64) for t in ("q", "k", "vt") for n in ("head", "row", "seq")]
+                + [("positions", C.c_void_p), ("positions_ld", C.c_int64), ("freqs", C.c_void_p)]
+                + [(n, C.c_void_p) for n in ("q_weight", "k_weight", "q_bias", "k_bias")]
+                + [(n, C.c_int32) for n in ("in_dtype", "out_dtype", "heads", "kv_heads",
+                                            "head_dim", "axes")]
+                + [("sections", C.c_int32 * 4)]
+                + [(n, C.c_int32) for n in ("pairing", "norm", "positions_f32")]
+                + [("q_scale", C.c_float), ("eps", C.c_float)])
 
 
 _P = C.c_void_p
@@ -131,6 +156,14 @@ _SIGS = {
     "acid_quantize_w4": (C.c_int, [_P, C.c_int32, C.c_int32, C.c_int32, _P, _P, _P]),
     "acid_linear_w4": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, _P,
                                  C.c_int64, _P, _P, _P, C.c_int32, C.c_int32, _P, C.c_int64, _P]),
+    "acid_quantize_fp8": (C.c_int, [C.c_int32, C.c_int64, C.c_int32, _P, C.c_int64, _P, C.c_int64,
+                                    _P, C.c_int64, _P]),
+    "acid_ln_modulate_fp8": (C.c_int, [C.c_int64, C.c_int32, _P, C.c_int64, _P, _P, C.c_int64, _P,
+                                       C.c_int64, _P, C.c_int64, _P]),
+    "acid_quantize_fp8_weight": (C.c_int, [_P, C.c_int32, C.c_int32, _P, _P, _P]),
+    "acid_linear_fp8_workspace_needed": (C.c_size_t, [C.c_int64, C.c_int32, C.c_int32]),
+    "acid_linear_fp8": (C.c_int, [C.POINTER(LinearFp8ArgsC), C.c_int64, C.c_int32, C.c_int32, _P]),
+    "acid_rotary_qkv": (C.c_int, [C.POINTER(RotaryQkvArgsC), C.c_int64, C.c_int64, _P]),
     "acid_block_forward": (C.c_int, [_P, C.c_int32, _P, _P, _P]),
 }
 

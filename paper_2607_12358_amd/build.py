@@ -26,7 +26,8 @@ BINDING = os.path.join(PKG, "_binding.so")
 ARCH = "gfx950"
 
 HIP_SOURCES = ["elementwise.hip", "temb.hip", "gemm.hip", "attention.hip", "runtime.hip",
-               "noalloc.hip", "linear_attention.hip", "residual_norm.hip", "linear_w4.hip"]
+               "noalloc.hip", "linear_attention.hip", "residual_norm.hip", "linear_w4.hip",
+               "quantize_fp8.hip", "linear_fp8.hip", "rotary.hip"]
 HOST_SOURCES = ["gate.cpp"]
 
 

@@ -1,7 +1,7 @@
-// Python module _binding: what the binding of the linear-attention block does for
-// each call, whose kernels for a few tokens take 3 to 7 us.
+// Python module _binding: what the binding of the linear-attention block and of the
+// 8-bit block does for each call, whose kernels for a few tokens take 3 to 7 us.
 //
-// at() and rows_at() give the address of a tensor that is as it has to be in 0.1
+// at(), rows_at() and heads_at() give the address of a tensor that is as it has to be in 0.1
 // us, where reading its shape, type, device, strides and address from Python
 // takes 0.6.  They look at tensors through DLPack's exchange interface (a table of
 // functions that torch offers as torch.Tensor.__dlpack_c_exchange_api__), so
@@ -42,11 +42,11 @@ struct Exchange {
 constexpr int32_t kRocm = 10;
 
 const Exchange* api = nullptr;
-PyObject *tensor_type = nullptr, *slow_at = nullptr, *slow_rows = nullptr;
+PyObject *tensor_type = nullptr, *slow_at = nullptr, *slow_rows = nullptr, *slow_heads = nullptr;
 struct {
   PyObject* dtype;
   uint8_t code, bits;
-} types[4];
+} types[8];
 int n_types = 0;
 
 // args: GPU, name, tensor, shape, dtype.  Whether the tensor is on that GPU, of
@@ -119,6 +119,18 @@ PyObject* rows_at(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return in_python(slow_rows, args, n);
 }
 
+PyObject* heads_at(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Tensor t;
+  if (look(args, n, &t) && (t.ndim == 3 || t.ndim == 4) &&
+      (t.shape[t.ndim - 1] == 1 || t.strides[t.ndim - 1] == 1)) {
+    const int64_t seq = t.ndim == 4 && t.shape[0] > 1 ? t.strides[0] : 0;
+    return Py_BuildValue("KLLL", (unsigned long long)((uintptr_t)t.data + t.byte_offset),
+                         (long long)t.strides[t.ndim - 3], (long long)t.strides[t.ndim - 2],
+                         (long long)seq);
+  }
+  return in_python(slow_heads, args, n);
+}
+
 // ------------------------------------------------------------- entry points
 
 // An argument of a C function: addresses as integers, None (NULL) or bytes.
@@ -163,7 +175,9 @@ PyObject* call(R (*f)(A...), PyObject* const* args, Py_ssize_t n) {
 // The library that ctypes has loaded gives the addresses.
 #define ENTRIES(E) \
   E(linear_attention_workspace_needed) E(linear_attention) E(linear_attention_step)               \
-  E(residual_norm) E(linear_w4) E(quantize_w4)
+  E(residual_norm) E(linear_w4) E(quantize_w4)                                                    \
+  E(quantize_fp8) E(ln_modulate_fp8) E(quantize_fp8_weight) E(linear_fp8_workspace_needed)        \
+  E(linear_fp8) E(rotary_qkv)
 #define ENTRY(name)                                                       \
   decltype(&acid_##name) name##_address = nullptr;                        \
   PyObject* name(PyObject*, PyObject* const* args, Py_ssize_t n) {        \
@@ -172,13 +186,13 @@ PyObject* call(R (*f)(A...), PyObject* const* args, Py_ssize_t n) {
 ENTRIES(ENTRY)
 #undef ENTRY
 
-// bind(exchange capsule or None, tensor type, Python's at, Python's rows_at,
+// bind(exchange capsule or None, tensor type, Python's at, rows_at and heads_at,
 // ((dtype, code, bits), ..), {entry point: address}): before the first call of
 // the others.
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *capsule, *type, *py_at, *py_rows, *dtypes, *entries;
-  if (!PyArg_ParseTuple(args, "OO!OOO!O!", &capsule, &PyType_Type, &type, &py_at, &py_rows,
-                        &PyTuple_Type, &dtypes, &PyDict_Type, &entries))
+  PyObject *capsule, *type, *py_at, *py_rows, *py_heads, *dtypes, *entries;
+  if (!PyArg_ParseTuple(args, "OO!OOOO!O!", &capsule, &PyType_Type, &type, &py_at, &py_rows,
+                        &py_heads, &PyTuple_Type, &dtypes, &PyDict_Type, &entries))
     return nullptr;
 #define ENTRY(name)                                                                         \
   if (PyObject* address = PyDict_GetItemString(entries, "acid_" #name))                     \
@@ -192,8 +206,8 @@ PyObject* bind(PyObject*, PyObject* args) {
     if (!x) return nullptr;
     if (x->major != 1 || !x->look) x = nullptr;  // an interface of another layout
   }
-  if (PyTuple_GET_SIZE(dtypes) > 4) {
-    PyErr_SetString(PyExc_ValueError, "at most four dtypes");
+  if (PyTuple_GET_SIZE(dtypes) > 8) {
+    PyErr_SetString(PyExc_ValueError, "at most eight dtypes");
     return nullptr;
   }
   n_types = 0;
@@ -208,9 +222,11 @@ PyObject* bind(PyObject*, PyObject* args) {
   Py_INCREF(type);
   Py_INCREF(py_at);
   Py_INCREF(py_rows);
+  Py_INCREF(py_heads);
   tensor_type = type;
   slow_at = py_at;
   slow_rows = py_rows;
+  slow_heads = py_heads;
   api = x;
   return PyBool_FromLong(x != nullptr);
 }
@@ -221,6 +237,8 @@ PyMethodDef methods[] = {
      "Address of a contiguous tensor, or None: (gpu, name, tensor, shape, dtype)."},
     {"rows_at", (PyCFunction)(void (*)())rows_at, METH_FASTCALL,
      "(address, row stride) of a matrix: (gpu, name, tensor, shape, dtype)."},
+    {"heads_at", (PyCFunction)(void (*)())heads_at, METH_FASTCALL,
+     "(address, head, row and sequence stride) of heads: (gpu, name, tensor, shape, dtype)."},
 #define ENTRY(name) {#name, (PyCFunction)(void (*)())name, METH_FASTCALL, "acid_" #name},
     ENTRIES(ENTRY)
 #undef ENTRY
