@@ -624,8 +624,8 @@ typedef struct {
 
 /* y = a w^T + bias with the rows' and the weights' scales, accumulated in fp32;
  * out = y (BIAS), GELU_tanh(y) (BIAS_GELU), residual + gate (.) y (GATE_RESIDUAL).  Any M
- * from a single row on (<= 2^24) and any N; K a multiple of 16, K and N <= 2^22; a_ld <
- * 2^24.  Plain and GELU outputs in fp32 come from exact products and fp32 sums; bf16 ones
+ * from a single row on (<= 2^24) and any N; K a multiple of 16, K and N <= 2^22, ceil(M /
+ * 64) ceil(N / 64) < 2^23; a_ld < 2^24.  Plain and GELU outputs in fp32 come from exact products and fp32 sums; bf16 ones
  * and the gated y from the 8-bit matrix units, whose sums are about 1.4e-5 off.  out
  * lies apart from everything but the residual.  Workspace:
  * acid_linear_fp8_workspace_needed(...) bytes (0: may be NULL), ACID_ERR_SHAPE if
