@@ -15,6 +15,7 @@
 // for the operands' own.  Outputs in bf16, and updates of a residual, take them.
 // Plain fp32 outputs take the bf16 instruction on operands converted on the way, which
 // is exact: products and sums in fp32.
+#include <algorithm>
 #include <type_traits>
 
 #include "fp8.h"
@@ -30,8 +31,8 @@ struct Fp8Args {
   const float *a_scales, *w_scales, *bias, *gate, *residual;
   void* out;
   int64_t a_ld, a_scales_ld, residual_ld, out_ld;
-  int32_t M, N, K, groups, kind;
-  bool vec;  // 16 bytes of outputs (and residual) may be read and written at once
+  int32_t M, N, K, groups;
+  bool whole;  // whole blocks of inputs, 16 bytes of outputs (and residual) at once
 };
 
 // Sixteen e4m3 values as bf16.
@@ -70,148 +71,257 @@ __device__ __forceinline__ void dma16_from(const void* p, uint32_t lds_byte) {
 }
 __device__ const u32x4 kZeros = {0, 0, 0, 0};
 
-// s_waitcnt vmcnt(n) alone
+// s_waitcnt vmcnt(n) alone, and lgkmcnt(0) alone
 #define WAIT_DMA(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (7 << 4) | (15 << 8) | (((n) >> 4) << 14))
 #define WAIT_LDS() __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14))
 
-// WT x WF waves, each with TT x FF blocks of 16 tokens x 16 outputs.
-template <int WT_, int WF_, int TT_, int FF_, int NST_, int OCC_>
+template <int N>
+using I = std::integral_constant<int, N>;
+template <int N, typename F>
+__device__ __forceinline__ void each(F f) {  // f(I<0>), ..
+  if constexpr (N > 0) {
+    each<N - 1>(f);
+    f(I<N - 1>{});
+  }
+}
+
+// WT x WF waves, each with TT x FF blocks of 16 tokens x 16 outputs; OCC workgroups
+// a CU.
+template <int WT_, int WF_, int TT_, int FF_, int OCC_>
 struct Tile {
-  static constexpr int WT = WT_, WF = WF_, TT = TT_, FF = FF_, NST = NST_, OCC = OCC_;
+  static constexpr int WT = WT_, WF = WF_, TT = TT_, FF = FF_, OCC = OCC_;
   static constexpr int TM = WT * TT * 16, TN = WF * FF * 16, WAVES = WT * WF;
-  static constexpr int STAGE = (TM + TN) * kFp8Group;      // bytes of a stage's operands
-  static constexpr int A_DMAS = TM / 32, DMAS = (TM + TN) / 32;  // of each of four waves
-  static constexpr int LDS = NST * (STAGE + TM * 4);
-  static_assert(WAVES >= 4 && TM % 32 == 0 && TN % 32 == 0 && FF % 2 == 0 && LDS <= 160 * 1024, "tile");
-  static_assert((DMAS + 1) * (NST - 1) <= 63, "loads in flight");
+  static constexpr int STAGE = (TM + TN) * kFp8Group;  // bytes of a stage's operands
+  static constexpr int LDS = 2 * (STAGE + TM * 4);
+  // A load fills 8 rows of 128 bytes.  A stage's part 0: the tokens, the first half of
+  // each wave's outputs, the tokens' scales (one load of wave 0); part 1: the second
+  // halves.  Loads of a wave:
+  static constexpr int LOADS_A = TM / 8 / WAVES, LOADS_W = TN / 16 / WAVES, LOADS0 = LOADS_A + LOADS_W;
+  // The eight rows of the outputs' tile that load i of wave w takes of its part's half are
+  // 8 (rows_of(i) + rows_of_wave(w)) .. in part 0, FF of them further in part 1.
+  static constexpr int rows_of(int i) { return WAVES >= FF ? i * (WAVES / FF) * 2 * FF : i / (FF / WAVES) * 2 * FF + i % (FF / WAVES) * WAVES; }
+  static __device__ int rows_of_wave(int w) { return WAVES >= FF ? w / FF * 2 * FF + w % FF : w; }
+  static_assert(WAVES % 4 == 0 && (WAVES % FF == 0 || FF % WAVES == 0) && FF % 4 == 0, "tile");
+  static_assert(TM % (8 * WAVES) == 0 && TN % (16 * WAVES) == 0 && TM <= 256, "loads");
+  static_assert(LDS * OCC <= 160 * 1024 && WAVES * OCC <= 32, "workgroups a CU");
 };
 
-// `rows` rows of COLS sums that lie in LDS, out: rows from m on, outputs from n on.
-template <typename Out, int KIND, int COLS>
-__device__ __forceinline__ void put_rows(const Fp8Args& a, uint32_t lds, int rows, int64_t m, int n, int lane) {
-  constexpr int EACH = 16 / sizeof(Out), LANES = COLS / EACH, STEP = 64 / LANES, SLOTS = COLS / 4;
-  const int r0 = lane / LANES, c = lane % LANES * EACH;
-  n += c;
-  const int left = (int)(a.M - m < rows ? a.M - m : rows);
-  if (n >= a.N) return;
-  float bias[EACH], gate[EACH];
+// Outputs of one tile, a wave's blocks of 16 tokens x 16 outputs out of its sums: lane l has
+// outputs 4 (l / 16) .. + 3 of token l % 16.
+// Whole 16 bytes: fp32 as they are; two bf16 blocks side by side exchange halves between
+// neighbouring rows of 16 lanes, so that each lane has eight outputs of one of them.
+template <typename Out, int KIND, bool GENERAL, int TT, int FF>
+__device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT], int64_t m0, int n0, int lane) {
+  const int lr = lane & 15, lg = lane >> 4;
+  auto column = [&](const float* v, int f) {  // of this lane's four outputs
+    f32x4 x;
 #pragma unroll
-  for (int e = 0; e < EACH; ++e) {
-    const int ne = n + e < a.N ? n + e : a.N - 1;
-    bias[e] = a.bias ? a.bias[ne] : 0.f;
-    gate[e] = KIND == ACID_EPI_GATE_RESIDUAL ? a.gate[ne] : 0.f;
-  }
-  for (int r = r0; r < left; r += STEP) {
-    float y[EACH];
-#pragma unroll
-    for (int q = 0; q < EACH / 4; ++q) {
-      const f32x4 v = __builtin_bit_cast(f32x4, lds16(lds + r * (COLS * 4) + ((c / 4 + q) ^ (r & 15)) % SLOTS * 16));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[4 * q + e] = v[e];
+    for (int r = 0; r < 4; ++r) {
+      const int n = n0 + f * 16 + 4 * lg + r;
+      x[r] = v[n < a.N ? n : a.N - 1];
     }
+    return x;
+  };
+  auto finish = [&](f32x4 y, const f32x4& bias, const f32x4& gate, const f32x4& old) {
+    y += bias;
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) {
-      y[e] += bias[e];
-      if constexpr (KIND == ACID_EPI_BIAS_GELU) y[e] = std::is_same_v<Out, bf16> ? gelu_tanh_fast(y[e]) : gelu_tanh(y[e]);
+    for (int r = 0; r < 4; ++r) {
+      if constexpr (KIND == ACID_EPI_BIAS_GELU) y[r] = std::is_same_v<Out, bf16> ? gelu_tanh_fast(y[r]) : gelu_tanh(y[r]);
+      if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) y[r] = fmaf(gate[r], y[r], old[r]);
     }
-    Out* dst = (Out*)a.out + (m + r) * a.out_ld + n;
-    const float* old = a.residual + (m + r) * a.residual_ld + n;
-    if (a.vec) {
-      if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) {
-        const f32x4 h = *reinterpret_cast<const f32x4*>(old);
+    return y;
+  };
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (GENERAL) {
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) y[e] = fmaf(gate[e], y[e], h[e]);
-      }
-      if constexpr (std::is_same_v<Out, bf16>) {
-        bf16x8 b;
+    for (int f = 0; f < FF; ++f) {
+      const f32x4 bias = a.bias ? column(a.bias, f) : zero;
+      const f32x4 gate = KIND == ACID_EPI_GATE_RESIDUAL ? column(a.gate, f) : zero;
+      const int n = n0 + f * 16 + 4 * lg;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) b[e] = (bf16)y[e];
-        *reinterpret_cast<bf16x8*>(dst) = b;
-      } else {
-        *reinterpret_cast<f32x4*>(dst) = f32x4{y[0], y[1], y[2], y[3]};
-      }
-    } else {
+      for (int t = 0; t < TT; ++t) {
+        const int64_t m = m0 + t * 16 + lr;
+        f32x4 old = zero;
+        if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) {
+          const float* at = a.residual + (m < a.M ? m : a.M - 1) * a.residual_ld;
 #pragma unroll
-      for (int e = 0; e < EACH; ++e)
-        if (n + e < a.N) {
-          if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) y[e] = fmaf(gate[e], y[e], old[e]);
-          dst[e] = (Out)y[e];
+          for (int r = 0; r < 4; ++r) old[r] = at[n + r < a.N ? n + r : a.N - 1];
         }
+        const f32x4 y = finish(acc[f][t], bias, gate, old);
+        if (m < a.M) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < a.N) ((Out*)a.out)[m * a.out_ld + n + r] = (Out)y[r];
+        }
+      }
+    }
+  } else if constexpr (std::is_same_v<Out, bf16>) {
+    const int64_t at = (int64_t)lr * a.out_ld + (lg & 1) * 16 + (lg & 2) * 4;
+    bf16* out = (bf16*)a.out + m0 * a.out_ld + n0 + at;
+    const int left_m = (int)(a.M - m0 < TT * 16 ? a.M - m0 : TT * 16) - lr, left_n = a.N - n0 - (int)((lg & 1) * 16 + (lg & 2) * 4);
+#pragma unroll
+    for (int f = 0; f < FF; f += 2) {
+      f32x4 bias[2] = {zero, zero};
+      if (a.bias) {
+        bias[0] = column(a.bias, f);
+        bias[1] = column(a.bias, f + 1);
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        uint32_t w[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const f32x4 y = finish(acc[f + i][t], bias[i], zero, zero);
+#pragma unroll
+          for (int r = 0; r < 2; ++r) w[i][r] = __builtin_bit_cast(uint32_t, bf16x2{(bf16)y[2 * r], (bf16)y[2 * r + 1]});
+        }
+        const auto lo = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false);
+        const auto hi = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
+        if (t * 16 < left_m && f * 16 < left_n)
+          *reinterpret_cast<u32x4*>(out + (int64_t)(t * 16) * a.out_ld + f * 16) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+      }
+    }
+  } else {
+    const int left_m = (int)(a.M - m0 < TT * 16 ? a.M - m0 : TT * 16) - lr, left_n = a.N - n0 - 4 * lg;
+    float* out = (float*)a.out + (m0 + lr) * a.out_ld + n0 + 4 * lg;
+    // the residual's values, AHEAD blocks ahead
+    constexpr int AHEAD = KIND == ACID_EPI_GATE_RESIDUAL ? 5 : 1, BLOCKS = FF * TT;
+    f32x4 old[AHEAD];
+    auto read_old = [&](int i) {
+      old[i % AHEAD] = zero;
+      if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) {
+        const int f = i / TT, t = i % TT;
+        const int64_t m = m0 + lr + (t * 16 < left_m ? t * 16 : left_m - 1);
+        const int n = f * 16 < left_n ? n0 + 4 * lg + f * 16 : a.N - 4;
+        if (left_m > 0) old[i % AHEAD] = *reinterpret_cast<const f32x4*>(a.residual + m * a.residual_ld + n);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read_old(i);
+    f32x4 bias, gate;
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i) {
+      const int f = i / TT, t = i % TT;
+      if (t == 0) {
+        bias = a.bias ? column(a.bias, f) : zero;
+        gate = KIND == ACID_EPI_GATE_RESIDUAL ? column(a.gate, f) : zero;
+      }
+      const f32x4 y = finish(acc[f][t], bias, gate, old[i % AHEAD]);
+      if (i + AHEAD < BLOCKS) read_old(i + AHEAD);
+      if (t * 16 < left_m && f * 16 < left_n)
+        *reinterpret_cast<f32x4*>(out + (int64_t)(t * 16) * a.out_ld + f * 16) = y;
     }
   }
 }
 
-// One output tile a workgroup.  A stage is one block of 128 inputs: a TM x 128
-// and a TN x 128 byte tile and the tokens' scales, loaded straight into LDS (four
-// waves issue the loads) NST - 1 stages ahead.  Row r's 16-byte chunk c lies at
-// slot c ^ (r / 2 % 8), so that sixteen rows of one chunk cover all 64 banks.
-// Inputs past K are loaded as zeros, rows past M and N as copies of the last.
-// A lane's operand of a 16 x 16 x 128 product is chunks g and g + 4 (g its row of 16
-// lanes) of both tiles' rows: any order of the inputs will do, if it is the same.
-template <typename Out, int KIND, bool EXACT, typename T>
-__global__ __launch_bounds__(64 * T::WAVES, T::OCC) void fp8_tile_kernel(Fp8Args a) {
-  constexpr int TT = T::TT, FF = T::FF, TM = T::TM, TN = T::TN, NST = T::NST, DMAS = T::DMAS;
+// Output tiles, a workgroup's one after the other; their stages form one stream.  A
+// stage is one block of 128 inputs: a TM x 128 and a TN x 128 byte tile and the tokens'
+// scales, loaded straight into one of two buffers in LDS.  Two barriers a stage: each frees
+// what all waves have read, a half of its buffer (part 0, then part 1), which is then
+// filled for the stage after the next, one load at a time between the products; so
+// loads run one and a half stages ahead, into the next tile.  (All at once behind
+// the barrier, they hold back the waves that issue them: see below.)
+// Row r's 16-byte chunk c lies at slot c ^ (r / 2 % 8), so that sixteen rows of one
+// chunk cover all 64 banks.  Rows past M and N are copies of the last.  A lane's operand of
+// a 16 x 16 x 128 product is chunks g and g + 4 (g its row of 16 lanes) of both tiles'
+// rows: any order of the inputs will do, if it is the same.
+// GENERAL: K that is no whole blocks, or outputs that are no whole 16 bytes.  The
+// short block comes first, its missing inputs loaded as zeros.
+template <typename Out, int KIND, bool EXACT, bool GENERAL, typename T>
+__global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile_kernel(Fp8Args a) {
+  constexpr int TT = T::TT, FF = T::FF, TM = T::TM, TN = T::TN, HALF = FF / 2 * TT;
   __shared__ __attribute__((aligned(1024))) uint8_t lds_tiles[T::LDS];
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)lds_tiles);
-  const uint32_t lds_scales = lds0 + NST * T::STAGE;
+  const uint32_t lds_scales = lds0 + 2 * T::STAGE;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wt = wave % T::WT, wf = wave / T::WT, lr = lane & 15, lg = lane >> 4;
-
-  const int tiles_n = (a.N + TN - 1) / TN;
+  const int NS = a.groups, tiles_n = (a.N + TN - 1) / TN;
   const uint32_t tiles_m = (a.M + TM - 1) / TM, tiles = tiles_m * tiles_n;
-  int64_t tm;
-  int tn;
-  tile_coords(xcd_remap(blockIdx.x, tiles), tiles_m, tiles_n, tm, tn);
-  const int64_t m0 = tm * TM;
-  const int n0 = tn * TN, NS = a.groups;
+  const int tail = GENERAL ? a.K % kFp8Group : 0;  // inputs of the short block, 0: none
 
-  // loads of a stage: DMA i of wave w < 4 takes rows 32 i + 8 w .. + 7 of the tiles
+  // ---- loads.  Where the next stage to be loaded lies:
   const int chunk = ((lane & 7) ^ lg ^ (4 * (wave & 1))) * 16;
-  const uint32_t row0 = 8 * wave + (lane >> 3);
   const uint32_t a_ld = (uint32_t)a.a_ld, w_ld = (uint32_t)a.K;
-  const uint32_t a_last = (uint32_t)(a.M - 1 - m0 < TM ? a.M - 1 - m0 : TM - 1) * a_ld;
-  const uint32_t w_last = (uint32_t)(a.N - 1 - n0 < TN ? a.N - 1 - n0 : TN - 1) * w_ld;
-  const uint64_t a_base = uniform_ptr(a.a + m0 * a.a_ld), w_base = uniform_ptr(a.w + (int64_t)n0 * a.K);
-  const uint32_t s_off = (uint32_t)(4 * lane < a.M - 1 - m0 ? 4 * lane : ((a.M - 1 - m0) & ~3)) * 4;
-  const uint64_t s_base = uniform_ptr(a.a_scales + m0);
-  const int tail = a.K % kFp8Group;  // inputs of the last block, 0: all
-  auto issue = [&](int st, uint32_t buf) {
-    uint32_t row_off = row0 * a_ld, w_off = row0 * w_ld;
-    asm volatile("" : "+v"(row_off), "+v"(w_off));  // not the offsets of all loads, kept in registers
-    const uint32_t k0 = (uint32_t)st * kFp8Group, at0 = lds0 + buf * T::STAGE + (uint32_t)wave * 1024;
-    if (tail && st == NS - 1) {
-      const bool in = chunk < tail;
-#pragma unroll 1
-      for (int i = 0; i < DMAS; ++i) {
-        const bool is_a = i < T::A_DMAS;
-        const uint32_t off = is_a ? min(row_off + i * 32 * a_ld, a_last) : min(w_off + (i - T::A_DMAS) * 32 * w_ld, w_last);
-        const uint8_t* at = reinterpret_cast<const uint8_t*>((is_a ? a_base : w_base) + k0) + off + chunk;
-        dma16_from(in ? at : reinterpret_cast<const uint8_t*>(&kZeros), at0 + i * 4096);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < DMAS; ++i) {
-        const bool is_a = i < T::A_DMAS;
-        const uint32_t off = is_a ? min(row_off + i * 32 * a_ld, a_last) : min(w_off + (i - T::A_DMAS) * 32 * w_ld, w_last);
-        dma16((is_a ? a_base : w_base) + k0, off + chunk, at0 + i * 4096);
-      }
+  const uint32_t a_row = (uint32_t)(8 * wave + (lane >> 3)) * a_ld;
+  const uint32_t w_row = (uint32_t)(8 * T::rows_of_wave(wave) + (lane >> 3)) * w_ld;
+  uint64_t a_from, w_from, s_from;  // its block
+  const float* sw_from;             // its scale of this wave's outputs
+  uint32_t a_last, w_last, s_off;   // of its tile
+  uint32_t next_tile = blockIdx.x;
+  int next_block = 0;               // of that tile's order; < 0 : its short block
+  auto enter_tile = [&]() {
+    int64_t tm;
+    int tn;
+    tile_coords(xcd_remap(next_tile < tiles ? next_tile : blockIdx.x, tiles), tiles_m, tiles_n, tm, tn);
+    const int64_t m0 = tm * TM;
+    const int n0 = tn * TN;
+    a_last = (uint32_t)(a.M - 1 - m0 < TM ? a.M - 1 - m0 : TM - 1) * a_ld;
+    w_last = (uint32_t)(a.N - 1 - n0 < TN ? a.N - 1 - n0 : TN - 1) * w_ld;
+    s_off = (uint32_t)(4 * lane < a.M - 1 - m0 ? 4 * lane : ((a.M - 1 - m0) & ~3)) * 4;
+    next_block = 0;
+    const int first = tail ? NS - 1 : 0;
+    a_from = uniform_ptr(a.a + m0 * a.a_ld) + (uint32_t)first * kFp8Group;
+    w_from = uniform_ptr(a.w + (int64_t)n0 * a.K) + (uint32_t)first * kFp8Group;
+    s_from = uniform_ptr(a.a_scales + m0) + (uint64_t)first * a.a_scales_ld * 4;
+    sw_from = a.w_scales + (int64_t)(min(n0 + wf * (FF * 16), a.N - 1) / kFp8Group) * NS + first;
+  };
+  auto leave_stage = [&]() {  // all loads of a stage have been issued
+    if (++next_block == NS) {
+      next_tile += gridDim.x;
+      enter_tile();
+      return;
     }
-    if (wave == 0 && lane < TM / 4)
-      dma16(s_base + (uint64_t)st * a.a_scales_ld * 4, s_off, lds_scales + buf * (TM * 4));
+    if (tail && next_block == 1) {  // from the short block to the first
+      a_from -= (uint32_t)(NS - 1) * kFp8Group;
+      w_from -= (uint32_t)(NS - 1) * kFp8Group;
+      s_from -= (uint64_t)(NS - 1) * a.a_scales_ld * 4;
+      sw_from -= NS - 1;
+    } else {
+      a_from += kFp8Group;
+      w_from += kFp8Group;
+      s_from += (uint64_t)a.a_scales_ld * 4;
+      sw_from += 1;
+    }
   };
-  // all but the `stages` youngest stages of this wave's loads have landed
-  auto landed = [&](auto stages) {
-    constexpr int S = decltype(stages)::value;
-    if (wave == 0) WAIT_DMA((DMAS + 1) * S);
-    else WAIT_DMA(DMAS * S);
+  auto copy = [&](uint64_t from, uint32_t off, uint32_t at) {
+    if (GENERAL && tail && next_block == 0)
+      dma16_from(chunk < tail ? reinterpret_cast<const uint8_t*>(from) + off : reinterpret_cast<const uint8_t*>(&kZeros), at);
+    else
+      dma16(from, off, at);
+  };
+  auto load = [&](auto part, auto index, uint32_t buf) {
+    constexpr int PART = decltype(part)::value, i = decltype(index)::value;
+    const uint32_t to = lds0 + buf * T::STAGE;
+    if constexpr (PART == 0 && i < T::LOADS_A) {
+      const uint32_t off = min(a_row + i * 8 * T::WAVES * a_ld, a_last) + chunk;
+      copy(a_from, off, to + (uint32_t)(i * T::WAVES + wave) * 1024);
+    } else if constexpr (PART == 0 && i == T::LOADS0) {
+      if (wave == 0 && lane < TM / 4) dma16(s_from, s_off, lds_scales + buf * (TM * 4));
+    } else {
+      constexpr int rows = T::rows_of(PART ? i : i - T::LOADS_A) + PART * FF;
+      const uint32_t off = min(w_row + 8 * rows * w_ld, w_last) + chunk;
+      copy(w_from, off, to + TM * kFp8Group + (uint32_t)(rows + T::rows_of_wave(wave)) * 1024);
+    }
+  };
+  // a part's loads whose turn is slot S of SLOTS
+  auto issue = [&](auto part, auto slot, auto slots, uint32_t buf) {
+    constexpr int PART = decltype(part)::value, S = decltype(slot)::value, N = decltype(slots)::value;
+    constexpr int LOADS = PART ? T::LOADS_W : T::LOADS0 + 1;
+    each<LOADS>([&](auto index) {
+      if constexpr (decltype(index)::value * N / LOADS == S) load(part, index, buf);
+    });
+  };
+  // All but this wave's youngest loads, of so many parts 0 and 1, have landed.  (What else is in
+  // flight, outputs of the last tile, makes the wait longer.)
+  auto landed = [&](auto parts0, auto parts1) {
+    constexpr int N0 = decltype(parts0)::value, N = T::LOADS0 * N0 + T::LOADS_W * decltype(parts1)::value;
+    static_assert(N + N0 <= 63, "loads in flight");
+    if (wave == 0) WAIT_DMA(N + N0);
+    else WAIT_DMA(N);
   };
 
-  // the outputs' scales, one stage a lane, 64 stages at a time
-  const int nb = min(n0 + wf * (FF * 16), a.N - 1) / kFp8Group;
-  const float* sw_at = a.w_scales + (int64_t)nb * a.groups;
-  float sw = sw_at[min(lane, NS - 1)];
-
+  // ---- operands
   const uint32_t swz = (uint32_t)((lg ^ (lr >> 1)) * 16);
   const uint32_t a_at = lds0 + (uint32_t)(wt * TT * 16 + lr) * kFp8Group + swz;
   const uint32_t w_at = lds0 + (uint32_t)(TM + wf * FF * 16 + lr) * kFp8Group + swz;
@@ -219,136 +329,137 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC) void fp8_tile_kernel(Fp8Args
   auto read = [&](uint32_t at, int block) {
     return Pair{{lds16(at + block * 2048), lds16((at ^ 64) + block * 2048)}};
   };
-
   f32x4 acc[FF][TT], part[TT];
   Pair fa[TT], fw[2];
   float s_old[TT], s_now[TT], s_next[TT];
-  auto main_loop = [&](auto issues) {
-  constexpr bool DMA = decltype(issues)::value;
-  if constexpr (DMA) {
-#pragma unroll
-    for (int st = 0; st < NST; ++st)
-      if (st < NS) issue(st, st);
-    if (NS >= NST) landed(std::integral_constant<int, NST - 1>{});
-    else WAIT_DMA(0);
-  }
+
+  // by way of the scalar cache: nothing that the loads in flight would be waited for
+  auto outputs_scale = [&]() {
+    return *(__attribute__((address_space(4))) const float*)uniform_ptr(sw_from);
+  };
+  enter_tile();
+  float sw_next = outputs_scale();
+  issue(I<0>{}, I<0>{}, I<1>{}, 0);
+  issue(I<1>{}, I<0>{}, I<1>{}, 0);
+  leave_stage();
+  issue(I<0>{}, I<0>{}, I<1>{}, 1);
+  each<TT>([&](auto slot) { issue(I<1>{}, slot, I<HALF>{}, 1); });  // the rest: within the first stage
+  landed(I<1>{}, I<1>{});  // part 0 of the first stage
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
   for (int t = 0; t < TT; ++t) {
-#pragma unroll
-    for (int f = 0; f < FF; ++f) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     part[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     fa[t] = read(a_at, t);
-    s_old[t] = 0.f;
     s_now[t] = 0.f;
     s_next[t] = lds4(s_at + t * 64);
   }
   fw[0] = read(w_at, 0);
 
-  uint32_t buf = 0, nxt = NST == 1 ? 0 : 1;
-  for (int st = 0; st < NS; ++st) {
-    if (st && st % 64 == 0) sw = sw_at[min(st + lane, NS - 1)];
-    const float sw_now = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sw), st % 64));
+  uint32_t buf = 0;
+  for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    int64_t tm;
+    int tn;
+    tile_coords(xcd_remap(tile, tiles), tiles_m, tiles_n, tm, tn);
+    const int64_t mw = tm * TM + wt * TT * 16;
+    const int nw = tn * TN + wf * FF * 16;
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
-      s_old[t] = s_now[t];
-      s_now[t] = s_next[t] * sw_now;
+      s_now[t] = 0.f;  // what is left in `part` belongs to the last tile
+#pragma unroll
+      for (int f = 0; f < FF; ++f) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      part[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const uint32_t cur_off = buf * T::STAGE, nxt_off = nxt * T::STAGE;
-#pragma unroll
-    for (int f = 0; f < FF; ++f) {
-      if (f + 1 < FF) {
-        fw[(f + 1) & 1] = read(w_at + cur_off, f + 1);
-      } else {
-        WAIT_LDS();  // the stage's last operands have arrived
-        if constexpr (DMA) {
-          if (st + NST - 1 < NS) landed(std::integral_constant<int, NST - 2>{});
-          else WAIT_DMA(0);
-        }
-        __builtin_amdgcn_s_barrier();  // the next stage has landed, and this one's tiles are free
-        asm volatile("" ::: "memory");
-        fw[0] = read(w_at + nxt_off, 0);  // past the last stage: read and dropped
-#pragma unroll
-        for (int t = 0; t < TT; ++t) s_next[t] = lds4(s_at + nxt * (TM * 4) + t * 64);
-      }
-      __builtin_amdgcn_sched_barrier(0);
+    for (int st = 0; st < NS; ++st) {
+      const uint32_t nxt = buf ^ 1, cur_off = buf * T::STAGE, nxt_off = nxt * T::STAGE;
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
-        const int pf = (f + FF - 1) % FF;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          acc[pf][t][r] = fmaf(f == 0 ? s_old[t] : s_now[t], part[t][r], acc[pf][t][r]);
-        asm volatile("" : "+v"(acc[pf][t]));  // here, not where the loop ends
-        if constexpr (EXACT) {
-          f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            bf16x8 bw[2], ba[2];
-            to_bf16(fw[f & 1].v[j], bw);
-            to_bf16(fa[t].v[j], ba);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-              sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i], ba[i], sum, 0, 0, 0);
-          }
-          part[t] = sum;
-        } else {
-          part[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-              __builtin_bit_cast(i32x8, fw[f & 1]), __builtin_bit_cast(i32x8, fa[t]),
-              f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-        }
-        if (f + 1 == FF) fa[t] = read(a_at + nxt_off, t);
-        __builtin_amdgcn_sched_barrier(0);
+        s_old[t] = s_now[t];
+        s_now[t] = s_next[t] * sw_next;
       }
-      if constexpr (DMA)
-        if (f + 1 == FF && st + NST < NS) issue(st + NST, buf);
+      each<FF>([&](auto f_) {
+        constexpr int f = decltype(f_)::value;
+        if constexpr (f + 1 == FF / 2) {
+          sw_next = outputs_scale();
+          leave_stage();
+          WAIT_LDS();                   // this half's last operands have arrived
+          landed(I<1>{}, I<1>{});       // part 1 of this stage: the next one's are younger
+          __builtin_amdgcn_s_barrier();  // for all waves; part 0 of this buffer is free
+          asm volatile("" ::: "memory");
+        }
+        if constexpr (f + 1 < FF) {
+          fw[(f + 1) & 1] = read(w_at + cur_off, f + 1);
+        } else {
+          WAIT_LDS();
+          landed(I<1>{}, I<1>{});       // part 0 of the next stage: its part 1 and part 0 of the one after are younger
+          __builtin_amdgcn_s_barrier();  // part 1 of this buffer is free
+          asm volatile("" ::: "memory");
+          fw[0] = read(w_at + nxt_off, 0);
+#pragma unroll
+          for (int t = 0; t < TT; ++t) s_next[t] = lds4(s_at + nxt * (TM * 4) + t * 64);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        each<TT>([&](auto t_) {
+          constexpr int t = decltype(t_)::value, pf = (f + FF - 1) % FF;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            acc[pf][t][r] = fmaf(f == 0 ? s_old[t] : s_now[t], part[t][r], acc[pf][t][r]);
+          asm volatile("" : "+v"(acc[pf][t]));  // here, not where the loop ends
+          if constexpr (EXACT) {
+            f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              bf16x8 bw[2], ba[2];
+              to_bf16(fw[f & 1].v[j], bw);
+              to_bf16(fa[t].v[j], ba);
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i], ba[i], sum, 0, 0, 0);
+            }
+            part[t] = sum;
+          } else {
+            part[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                __builtin_bit_cast(i32x8, fw[f & 1]), __builtin_bit_cast(i32x8, fa[t]),
+                f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+          }
+          if constexpr (f + 1 == FF) fa[t] = read(a_at + nxt_off, t);
+          if constexpr (f + 1 >= FF / 2 && f + 1 < FF)
+            issue(I<0>{}, I<(f + 1 - FF / 2) * TT + t>{}, I<HALF>{}, buf);
+          else if constexpr (f + 1 == FF)
+            issue(I<1>{}, I<t>{}, I<HALF>{}, buf);
+          else
+            issue(I<1>{}, I<(f + 1) * TT + t>{}, I<HALF>{}, nxt);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
+      buf = nxt;
     }
-    buf = nxt;
-    nxt = nxt + 1 == NST ? 0 : nxt + 1;
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[FF - 1][t][r] = fmaf(s_now[t], part[t][r], acc[FF - 1][t][r]);
+    put_tile<Out, KIND, GENERAL, TT, FF>(a, acc, mw, nw, lane);
   }
-  };
-  if (wave < 4) main_loop(std::true_type{});
-  else main_loop(std::false_type{});
-#pragma unroll
-  for (int t = 0; t < TT; ++t)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) acc[FF - 1][t][r] = fmaf(s_now[t], part[t][r], acc[FF - 1][t][r]);
-
-  // Out by way of LDS, whole rows of the wave's outputs at a time: two blocks of tokens in
-  // a part of LDS that is this wave's alone (every load has landed, and what waves still
-  // read past the last stage is dropped).  The 16-byte slot s of token i is at s ^ i % 16.
-  constexpr int COLS = FF * 16, SLOTS = COLS / 4, PER = TT < 2 ? 1 : 2;
-  static_assert(T::WAVES * PER * 16 * COLS * 4 <= T::LDS && TT % PER == 0, "outputs by way of LDS");
-  const uint32_t mine = lds0 + (uint32_t)wave * (PER * 16 * COLS * 4);
-  const int nw = n0 + wf * COLS;
-#pragma unroll
-  for (int t = 0; t < TT; t += PER) {
-#pragma unroll
-    for (int p = 0; p < PER; ++p)
-#pragma unroll
-      for (int f = 0; f < FF; ++f)
-        *(__attribute__((address_space(3))) f32x4*)(mine + (p * 16 + lr) * (COLS * 4) + ((4 * f + lg) ^ lr) % SLOTS * 16) = acc[f][t + p];
-    asm volatile("" ::: "memory");
-    WAIT_LDS();
-    put_rows<Out, KIND, COLS>(a, mine, PER * 16, m0 + (wt * TT + t) * 16, nw, lane);
-    WAIT_LDS();
-    asm volatile("" ::: "memory");
-  }
+  WAIT_DMA(0);  // the loads past the last stage land before the LDS is another workgroup's
 }
 
 template <typename Out, int KIND, bool EXACT, typename T>
 hipError_t launch_tile(const Fp8Args& a, hipStream_t s) {
   const int64_t tiles = ((int64_t)a.M + T::TM - 1) / T::TM * ((a.N + T::TN - 1) / T::TN);
-  hipLaunchKernelGGL((fp8_tile_kernel<Out, KIND, EXACT, T>), dim3((unsigned)tiles), dim3(64 * T::WAVES), 0, s, a);
+  const dim3 grid((unsigned)std::min<int64_t>(tiles, device_cus() * T::OCC)), block(64 * T::WAVES);
+  if (a.whole)
+    hipLaunchKernelGGL((fp8_tile_kernel<Out, KIND, EXACT, false, T>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((fp8_tile_kernel<Out, KIND, EXACT, true, T>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
 template <typename Out, int KIND, bool EXACT>
 hipError_t launch(const Fp8Args& a, hipStream_t s) {
   if constexpr (EXACT)
-    return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, 4, 2, 1>>(a, s);
+    return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, 4, 1>>(a, s);
   else
-    return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, 8, 2, 1>>(a, s);
+    return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, 8, 1>>(a, s);
 }
 
 }  // namespace
@@ -422,11 +533,11 @@ acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t
     return set_error(ACID_ERR_INVALID_ARG, "fp8: workspace overlaps out");
   StreamDevice on;
   ACID_TRY(on.enter(stream));
-  const bool vec = N * os % 16 == 0 && p.out_ld * os % 16 == 0 && (uintptr_t)p.out % 16 == 0 &&
-                   (!update || (p.residual_ld % 4 == 0 && (uintptr_t)p.residual % 16 == 0));
+  const bool whole = K % kFp8Group == 0 && N * os % 16 == 0 && p.out_ld * os % 16 == 0 && (uintptr_t)p.out % 16 == 0 &&
+                     (!update || (p.residual_ld % 4 == 0 && (uintptr_t)p.residual % 16 == 0));
   const Fp8Args a = {(const uint8_t*)p.a, (const uint8_t*)p.w, p.a_scales, p.w_scales, p.bias, p.gate,
                      p.residual, p.out, p.a_ld, p.a_scales_ld, p.residual_ld, p.out_ld, (int32_t)M, N,
-                     K, (int32_t)groups, p.kind, vec};
+                     K, (int32_t)groups, whole};
   hipError_t e;
   if (p.out_dtype == ACID_BF16)
     e = p.kind == ACID_EPI_BIAS ? launch<bf16, ACID_EPI_BIAS, false>(a, stream)
