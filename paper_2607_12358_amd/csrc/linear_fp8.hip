@@ -92,7 +92,7 @@ struct Tile {
   static constexpr int WT = WT_, WF = WF_, TT = TT_, FF = FF_, OCC = OCC_;
   static constexpr int TM = WT * TT * 16, TN = WF * FF * 16, WAVES = WT * WF;
   static constexpr int STAGE = (TM + TN) * kFp8Group;  // bytes of a stage's operands
-  static constexpr int LDS = 2 * (STAGE + TM * 4);
+  static constexpr int LDS = 2 * (STAGE + TM * 4) + WAVES * FF * 16 * 8;  // .. and bias and gate
   // A load fills 8 rows of 128 bytes.  A stage's part 0: the tokens, the first half of
   // each wave's outputs, the tokens' scales (one load of wave 0); part 1: the second
   // halves.  Loads of a wave:
@@ -111,14 +111,20 @@ struct Tile {
 // Whole 16 bytes: fp32 as they are; two bf16 blocks side by side exchange halves between
 // neighbouring rows of 16 lanes, so that each lane has eight outputs of one of them.
 template <typename Out, int KIND, bool GENERAL, int TT, int FF>
-__device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT], int64_t m0, int n0, int lane) {
+__device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT], int64_t m0, int n0,
+                                         uint32_t columns, int lane) {
   const int lr = lane & 15, lg = lane >> 4;
-  auto column = [&](const float* v, int f) {  // of this lane's four outputs
-    f32x4 x;
+  auto column = [&](int which, int f) {  // bias (0) or gate (1) of this lane's four outputs
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (GENERAL) {
+      const float* v = which ? a.gate : a.bias;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int n = n0 + f * 16 + 4 * lg + r;
-      x[r] = v[n < a.N ? n : a.N - 1];
+      for (int r = 0; r < 4; ++r) {
+        const int n = n0 + f * 16 + 4 * lg + r;
+        if (v) x[r] = v[n < a.N ? n : a.N - 1];
+      }
+    } else {  // laid out in LDS when the tile began
+      x = __builtin_bit_cast(f32x4, lds16(columns + (which * FF + f) * 64 + lg * 16));
     }
     return x;
   };
@@ -135,8 +141,7 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
   if constexpr (GENERAL) {
 #pragma unroll
     for (int f = 0; f < FF; ++f) {
-      const f32x4 bias = a.bias ? column(a.bias, f) : zero;
-      const f32x4 gate = KIND == ACID_EPI_GATE_RESIDUAL ? column(a.gate, f) : zero;
+      const f32x4 bias = column(0, f), gate = KIND == ACID_EPI_GATE_RESIDUAL ? column(1, f) : zero;
       const int n = n0 + f * 16 + 4 * lg;
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
@@ -161,11 +166,7 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
     const int left_m = (int)(a.M - m0 < TT * 16 ? a.M - m0 : TT * 16) - lr, left_n = a.N - n0 - (int)((lg & 1) * 16 + (lg & 2) * 4);
 #pragma unroll
     for (int f = 0; f < FF; f += 2) {
-      f32x4 bias[2] = {zero, zero};
-      if (a.bias) {
-        bias[0] = column(a.bias, f);
-        bias[1] = column(a.bias, f + 1);
-      }
+      const f32x4 bias[2] = {column(0, f), column(0, f + 1)};
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
         uint32_t w[2][2];
@@ -178,14 +179,15 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
         const auto lo = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false);
         const auto hi = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
         if (t * 16 < left_m && f * 16 < left_n)
-          *reinterpret_cast<u32x4*>(out + (int64_t)(t * 16) * a.out_ld + f * 16) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+          __builtin_nontemporal_store(u32x4{lo[0], hi[0], lo[1], hi[1]},
+                                      reinterpret_cast<u32x4*>(out + (int64_t)(t * 16) * a.out_ld + f * 16));
       }
     }
   } else {
     const int left_m = (int)(a.M - m0 < TT * 16 ? a.M - m0 : TT * 16) - lr, left_n = a.N - n0 - 4 * lg;
     float* out = (float*)a.out + (m0 + lr) * a.out_ld + n0 + 4 * lg;
     // the residual's values, AHEAD blocks ahead
-    constexpr int AHEAD = KIND == ACID_EPI_GATE_RESIDUAL ? 5 : 1, BLOCKS = FF * TT;
+    constexpr int AHEAD = KIND == ACID_EPI_GATE_RESIDUAL ? 12 : 1, BLOCKS = FF * TT;
     f32x4 old[AHEAD];
     auto read_old = [&](int i) {
       old[i % AHEAD] = zero;
@@ -203,13 +205,13 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
     for (int i = 0; i < BLOCKS; ++i) {
       const int f = i / TT, t = i % TT;
       if (t == 0) {
-        bias = a.bias ? column(a.bias, f) : zero;
-        gate = KIND == ACID_EPI_GATE_RESIDUAL ? column(a.gate, f) : zero;
+        bias = column(0, f);
+        gate = KIND == ACID_EPI_GATE_RESIDUAL ? column(1, f) : zero;
       }
       const f32x4 y = finish(acc[f][t], bias, gate, old[i % AHEAD]);
       if (i + AHEAD < BLOCKS) read_old(i + AHEAD);
       if (t * 16 < left_m && f * 16 < left_n)
-        *reinterpret_cast<f32x4*>(out + (int64_t)(t * 16) * a.out_ld + f * 16) = y;
+        __builtin_nontemporal_store(y, reinterpret_cast<f32x4*>(out + (int64_t)(t * 16) * a.out_ld + f * 16));
     }
   }
 }
@@ -236,6 +238,7 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wt = wave % T::WT, wf = wave / T::WT, lr = lane & 15, lg = lane >> 4;
+  const uint32_t columns = lds_scales + 2 * TM * 4 + (uint32_t)wave * (FF * 128);  // bias, gate
   const int NS = a.groups, tiles_n = (a.N + TN - 1) / TN;
   const uint32_t tiles_m = (a.M + TM - 1) / TM, tiles = tiles_m * tiles_n;
   const int tail = GENERAL ? a.K % kFp8Group : 0;  // inputs of the short block, 0: none
@@ -245,19 +248,24 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
   const uint32_t a_ld = (uint32_t)a.a_ld, w_ld = (uint32_t)a.K;
   const uint32_t a_row = (uint32_t)(8 * wave + (lane >> 3)) * a_ld;
   const uint32_t w_row = (uint32_t)(8 * T::rows_of_wave(wave) + (lane >> 3)) * w_ld;
+  uint32_t a_off[T::LOADS_A], w_off[2][T::LOADS_W], s_off;  // of its tile's rows
   uint64_t a_from, w_from, s_from;  // its block
   const float* sw_from;             // its scale of this wave's outputs
-  uint32_t a_last, w_last, s_off;   // of its tile
   uint32_t next_tile = blockIdx.x;
   int next_block = 0;               // of that tile's order; < 0 : its short block
   auto enter_tile = [&]() {
     int64_t tm;
     int tn;
-    tile_coords(xcd_remap(next_tile < tiles ? next_tile : blockIdx.x, tiles), tiles_m, tiles_n, tm, tn);
+    tile_coords<4>(xcd_remap(next_tile < tiles ? next_tile : blockIdx.x, tiles), tiles_m, tiles_n, tm, tn);
     const int64_t m0 = tm * TM;
     const int n0 = tn * TN;
-    a_last = (uint32_t)(a.M - 1 - m0 < TM ? a.M - 1 - m0 : TM - 1) * a_ld;
-    w_last = (uint32_t)(a.N - 1 - n0 < TN ? a.N - 1 - n0 : TN - 1) * w_ld;
+    const uint32_t a_last = (uint32_t)(a.M - 1 - m0 < TM ? a.M - 1 - m0 : TM - 1) * a_ld;
+    const uint32_t w_last = (uint32_t)(a.N - 1 - n0 < TN ? a.N - 1 - n0 : TN - 1) * w_ld;
+    each<T::LOADS_A>([&](auto i) { a_off[i()] = min(a_row + i() * 8 * T::WAVES * a_ld, a_last) + chunk; });
+    each<T::LOADS_W>([&](auto i) {
+      w_off[0][i()] = min(w_row + 8 * T::rows_of(i()) * w_ld, w_last) + chunk;
+      w_off[1][i()] = min(w_row + 8 * (T::rows_of(i()) + FF) * w_ld, w_last) + chunk;
+    });
     s_off = (uint32_t)(4 * lane < a.M - 1 - m0 ? 4 * lane : ((a.M - 1 - m0) & ~3)) * 4;
     next_block = 0;
     const int first = tail ? NS - 1 : 0;
@@ -294,14 +302,12 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
     constexpr int PART = decltype(part)::value, i = decltype(index)::value;
     const uint32_t to = lds0 + buf * T::STAGE;
     if constexpr (PART == 0 && i < T::LOADS_A) {
-      const uint32_t off = min(a_row + i * 8 * T::WAVES * a_ld, a_last) + chunk;
-      copy(a_from, off, to + (uint32_t)(i * T::WAVES + wave) * 1024);
+      copy(a_from, a_off[i], to + (uint32_t)(i * T::WAVES + wave) * 1024);
     } else if constexpr (PART == 0 && i == T::LOADS0) {
       if (wave == 0 && lane < TM / 4) dma16(s_from, s_off, lds_scales + buf * (TM * 4));
     } else {
-      constexpr int rows = T::rows_of(PART ? i : i - T::LOADS_A) + PART * FF;
-      const uint32_t off = min(w_row + 8 * rows * w_ld, w_last) + chunk;
-      copy(w_from, off, to + TM * kFp8Group + (uint32_t)(rows + T::rows_of_wave(wave)) * 1024);
+      constexpr int j = PART ? i : i - T::LOADS_A, rows = T::rows_of(j) + PART * FF;
+      copy(w_from, w_off[PART][j], to + TM * kFp8Group + (uint32_t)(rows + T::rows_of_wave(wave)) * 1024);
     }
   };
   // a part's loads whose turn is slot S of SLOTS
@@ -331,7 +337,7 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
   };
   f32x4 acc[FF][TT], part[TT];
   Pair fa[TT], fw[2];
-  float s_old[TT], s_now[TT], s_next[TT];
+  float s_now[TT], s_next[TT];
 
   // by way of the scalar cache: nothing that the loads in flight would be waited for
   auto outputs_scale = [&]() {
@@ -344,23 +350,24 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
   leave_stage();
   issue(I<0>{}, I<0>{}, I<1>{}, 1);
   each<TT>([&](auto slot) { issue(I<1>{}, slot, I<HALF>{}, 1); });  // the rest: within the first stage
+  auto first_operands = [&](uint32_t buf) {
+    fw[0] = read(w_at + buf * T::STAGE, 0);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      fa[t] = read(a_at + buf * T::STAGE, t);
+      s_next[t] = lds4(s_at + buf * (TM * 4) + t * 64);
+    }
+  };
   landed(I<1>{}, I<1>{});  // part 0 of the first stage
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-#pragma unroll
-  for (int t = 0; t < TT; ++t) {
-    part[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    fa[t] = read(a_at, t);
-    s_now[t] = 0.f;
-    s_next[t] = lds4(s_at + t * 64);
-  }
-  fw[0] = read(w_at, 0);
+  first_operands(0);
 
   uint32_t buf = 0;
   for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     int64_t tm;
     int tn;
-    tile_coords(xcd_remap(tile, tiles), tiles_m, tiles_n, tm, tn);
+    tile_coords<4>(xcd_remap(tile, tiles), tiles_m, tiles_n, tm, tn);
     const int64_t mw = tm * TM + wt * TT * 16;
     const int nw = tn * TN + wf * FF * 16;
 #pragma unroll
@@ -370,15 +377,21 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
       for (int f = 0; f < FF; ++f) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       part[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    if constexpr (!GENERAL) {
+      const int n = min(nw + 4 * lane, a.N - 4);
+      if (lane < FF * 4) {
+        dma16_from(a.bias ? (const void*)(a.bias + n) : &kZeros, columns);
+        if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) dma16_from(a.gate + n, columns + FF * 64);
+      }
+    }
     for (int st = 0; st < NS; ++st) {
       const uint32_t nxt = buf ^ 1, cur_off = buf * T::STAGE, nxt_off = nxt * T::STAGE;
-#pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        s_old[t] = s_now[t];
-        s_now[t] = s_next[t] * sw_next;
-      }
       each<FF>([&](auto f_) {
         constexpr int f = decltype(f_)::value;
+        if constexpr (f == 1) {  // (the sums that are added in f == 0 are the last stage's)
+#pragma unroll
+          for (int t = 0; t < TT; ++t) s_now[t] = s_next[t] * sw_next;
+        }
         if constexpr (f + 1 == FF / 2) {
           sw_next = outputs_scale();
           leave_stage();
@@ -403,7 +416,7 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
           constexpr int t = decltype(t_)::value, pf = (f + FF - 1) % FF;
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            acc[pf][t][r] = fmaf(f == 0 ? s_old[t] : s_now[t], part[t][r], acc[pf][t][r]);
+            acc[pf][t][r] = fmaf(s_now[t], part[t][r], acc[pf][t][r]);
           asm volatile("" : "+v"(acc[pf][t]));  // here, not where the loop ends
           if constexpr (EXACT) {
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -438,7 +451,14 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[FF - 1][t][r] = fmaf(s_now[t], part[t][r], acc[FF - 1][t][r]);
-    put_tile<Out, KIND, GENERAL, TT, FF>(a, acc, mw, nw, lane);
+    if constexpr (!GENERAL) {
+      WAIT_DMA(T::LOADS0);  // bias and gate: this many loads were issued after them
+      asm volatile("" ::: "memory");
+    }
+    put_tile<Out, KIND, GENERAL, TT, FF>(a, acc, mw, nw, columns, lane);
+    WAIT_LDS();  // bias and gate have been read
+    asm volatile("" ::: "memory");
+    first_operands(buf);  // again: their registers held what is above
   }
   WAIT_DMA(0);  // the loads past the last stage land before the LDS is another workgroup's
 }
@@ -534,7 +554,8 @@ acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t
   StreamDevice on;
   ACID_TRY(on.enter(stream));
   const bool whole = K % kFp8Group == 0 && N * os % 16 == 0 && p.out_ld * os % 16 == 0 && (uintptr_t)p.out % 16 == 0 &&
-                     (!update || (p.residual_ld % 4 == 0 && (uintptr_t)p.residual % 16 == 0));
+                     (uintptr_t)p.bias % 16 == 0 &&
+                     (!update || (p.residual_ld % 4 == 0 && ((uintptr_t)p.residual | (uintptr_t)p.gate) % 16 == 0));
   const Fp8Args a = {(const uint8_t*)p.a, (const uint8_t*)p.w, p.a_scales, p.w_scales, p.bias, p.gate,
                      p.residual, p.out, p.a_ld, p.a_scales_ld, p.residual_ld, p.out_ld, (int32_t)M, N,
                      K, (int32_t)groups, whole};
