@@ -19,6 +19,7 @@
 #include <type_traits>
 
 #include "fp8.h"
+#include "fp8_form.h"
 #include "tiles.h"
 
 namespace acid {
@@ -31,7 +32,8 @@ struct Fp8Args {
   const float *a_scales, *w_scales, *bias, *gate, *residual;
   void* out;
   int64_t a_ld, a_scales_ld, residual_ld, out_ld;
-  int32_t M, N, K, groups;
+  float* partial;  // sums of parts of K, for fp8_reduce_kernel
+  int32_t M, N, K, groups, split;
   bool whole;  // whole blocks of inputs, 16 bytes of outputs (and residual) at once
 };
 
@@ -75,6 +77,8 @@ __device__ const u32x4 kZeros = {0, 0, 0, 0};
 #define WAIT_DMA(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (7 << 4) | (15 << 8) | (((n) >> 4) << 14))
 #define WAIT_LDS() __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14))
 
+constexpr int PARTIAL = -1;  // in the place of an epilogue: raw sums into a.partial
+
 template <int N>
 using I = std::integral_constant<int, N>;
 template <int N, typename F>
@@ -113,6 +117,7 @@ struct Tile {
 template <typename Out, int KIND, bool GENERAL, int TT, int FF>
 __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT], int64_t m0, int n0,
                                          uint32_t columns, int lane) {
+  asm volatile("" : "+v"(lane));  // nothing of this is kept in registers through the stages
   const int lr = lane & 15, lg = lane >> 4;
   auto column = [&](int which, int f) {  // bias (0) or gate (1) of this lane's four outputs
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -166,6 +171,7 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
     const int left_m = (int)(a.M - m0 < TT * 16 ? a.M - m0 : TT * 16) - lr, left_n = a.N - n0 - (int)((lg & 1) * 16 + (lg & 2) * 4);
 #pragma unroll
     for (int f = 0; f < FF; f += 2) {
+      __builtin_amdgcn_sched_barrier(0);  // (not all of the tile's bias at once)
       const f32x4 bias[2] = {column(0, f), column(0, f + 1)};
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
@@ -187,7 +193,7 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
     const int left_m = (int)(a.M - m0 < TT * 16 ? a.M - m0 : TT * 16) - lr, left_n = a.N - n0 - 4 * lg;
     float* out = (float*)a.out + (m0 + lr) * a.out_ld + n0 + 4 * lg;
     // the residual's values, AHEAD blocks ahead
-    constexpr int AHEAD = KIND == ACID_EPI_GATE_RESIDUAL ? 12 : 1, BLOCKS = FF * TT;
+    constexpr int AHEAD = KIND == ACID_EPI_GATE_RESIDUAL ? 10 : 1, BLOCKS = FF * TT;
     f32x4 old[AHEAD];
     auto read_old = [&](int i) {
       old[i % AHEAD] = zero;
@@ -216,7 +222,8 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
   }
 }
 
-// Output tiles, a workgroup's one after the other; their stages form one stream.  A
+// Output tiles, a workgroup's one after the other, or with PARTIAL parts of K of
+// them; their stages form one stream.  A
 // stage is one block of 128 inputs: a TM x 128 and a TN x 128 byte tile and the tokens'
 // scales, loaded straight into one of two buffers in LDS.  Two barriers a stage: each frees
 // what all waves have read, a half of its buffer (part 0, then part 1), which is then
@@ -240,7 +247,23 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
   const int wt = wave % T::WT, wf = wave / T::WT, lr = lane & 15, lg = lane >> 4;
   const uint32_t columns = lds_scales + 2 * TM * 4 + (uint32_t)wave * (FF * 128);  // bias, gate
   const int NS = a.groups, tiles_n = (a.N + TN - 1) / TN;
-  const uint32_t tiles_m = (a.M + TM - 1) / TM, tiles = tiles_m * tiles_n;
+  const uint32_t tiles_m = (a.M + TM - 1) / TM, tiles = tiles_m * tiles_n, items = tiles * a.split;
+  // A work item: tile (tm, tn), the blocks from `first` to before `end` of its order, where
+  // a short block is the first.  Parts outermost, so that neighbours share operands.
+  struct Item {
+    uint32_t index;
+    int64_t tm;
+    int tn, first, end;
+  };
+  auto item_at = [&](uint32_t i) {
+    Item r;
+    r.index = xcd_remap(i < items ? i : blockIdx.x, items);
+    const uint32_t part = KIND == PARTIAL ? r.index / tiles : 0;
+    tile_coords<4>(r.index - part * tiles, tiles_m, tiles_n, r.tm, r.tn);
+    r.first = KIND == PARTIAL ? (int)((int64_t)NS * part / a.split) : 0;
+    r.end = KIND == PARTIAL ? (int)((int64_t)NS * (part + 1) / a.split) : NS;
+    return r;
+  };
   const int tail = GENERAL ? a.K % kFp8Group : 0;  // inputs of the short block, 0: none
 
   // ---- loads.  Where the next stage to be loaded lies:
@@ -251,14 +274,12 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
   uint32_t a_off[T::LOADS_A], w_off[2][T::LOADS_W], s_off;  // of its tile's rows
   uint64_t a_from, w_from, s_from;  // its block
   const float* sw_from;             // its scale of this wave's outputs
-  uint32_t next_tile = blockIdx.x;
-  int next_block = 0;               // of that tile's order; < 0 : its short block
-  auto enter_tile = [&]() {
-    int64_t tm;
-    int tn;
-    tile_coords<4>(xcd_remap(next_tile < tiles ? next_tile : blockIdx.x, tiles), tiles_m, tiles_n, tm, tn);
-    const int64_t m0 = tm * TM;
-    const int n0 = tn * TN;
+  uint32_t next_item = blockIdx.x;
+  int next_block, next_end;         // of that item's order
+  auto enter_item = [&]() {
+    const Item it = item_at(next_item);
+    const int64_t m0 = it.tm * TM;
+    const int n0 = it.tn * TN;
     const uint32_t a_last = (uint32_t)(a.M - 1 - m0 < TM ? a.M - 1 - m0 : TM - 1) * a_ld;
     const uint32_t w_last = (uint32_t)(a.N - 1 - n0 < TN ? a.N - 1 - n0 : TN - 1) * w_ld;
     each<T::LOADS_A>([&](auto i) { a_off[i()] = min(a_row + i() * 8 * T::WAVES * a_ld, a_last) + chunk; });
@@ -267,17 +288,18 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
       w_off[1][i()] = min(w_row + 8 * (T::rows_of(i()) + FF) * w_ld, w_last) + chunk;
     });
     s_off = (uint32_t)(4 * lane < a.M - 1 - m0 ? 4 * lane : ((a.M - 1 - m0) & ~3)) * 4;
-    next_block = 0;
-    const int first = tail ? NS - 1 : 0;
+    next_block = it.first;
+    next_end = it.end;
+    const int first = !tail ? it.first : it.first ? it.first - 1 : NS - 1;
     a_from = uniform_ptr(a.a + m0 * a.a_ld) + (uint32_t)first * kFp8Group;
     w_from = uniform_ptr(a.w + (int64_t)n0 * a.K) + (uint32_t)first * kFp8Group;
     s_from = uniform_ptr(a.a_scales + m0) + (uint64_t)first * a.a_scales_ld * 4;
     sw_from = a.w_scales + (int64_t)(min(n0 + wf * (FF * 16), a.N - 1) / kFp8Group) * NS + first;
   };
   auto leave_stage = [&]() {  // all loads of a stage have been issued
-    if (++next_block == NS) {
-      next_tile += gridDim.x;
-      enter_tile();
+    if (++next_block == next_end) {
+      next_item += gridDim.x;
+      enter_item();
       return;
     }
     if (tail && next_block == 1) {  // from the short block to the first
@@ -343,7 +365,7 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
   auto outputs_scale = [&]() {
     return *(__attribute__((address_space(4))) const float*)uniform_ptr(sw_from);
   };
-  enter_tile();
+  enter_item();
   float sw_next = outputs_scale();
   issue(I<0>{}, I<0>{}, I<1>{}, 0);
   issue(I<1>{}, I<0>{}, I<1>{}, 0);
@@ -364,12 +386,10 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
   first_operands(0);
 
   uint32_t buf = 0;
-  for (uint32_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    int64_t tm;
-    int tn;
-    tile_coords<4>(xcd_remap(tile, tiles), tiles_m, tiles_n, tm, tn);
-    const int64_t mw = tm * TM + wt * TT * 16;
-    const int nw = tn * TN + wf * FF * 16;
+  for (uint32_t i = blockIdx.x; i < items; i += gridDim.x) {
+    const Item it = item_at(i);
+    const int64_t mw = it.tm * TM + wt * TT * 16;
+    const int nw = it.tn * TN + wf * FF * 16;
 #pragma unroll
     for (int t = 0; t < TT; ++t) {
       s_now[t] = 0.f;  // what is left in `part` belongs to the last tile
@@ -377,14 +397,14 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
       for (int f = 0; f < FF; ++f) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       part[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    if constexpr (!GENERAL) {
+    if constexpr (!GENERAL && KIND != PARTIAL) {
       const int n = min(nw + 4 * lane, a.N - 4);
       if (lane < FF * 4) {
         dma16_from(a.bias ? (const void*)(a.bias + n) : &kZeros, columns);
         if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) dma16_from(a.gate + n, columns + FF * 64);
       }
     }
-    for (int st = 0; st < NS; ++st) {
+    for (int st = it.first; st < it.end; ++st) {
       const uint32_t nxt = buf ^ 1, cur_off = buf * T::STAGE, nxt_off = nxt * T::STAGE;
       each<FF>([&](auto f_) {
         constexpr int f = decltype(f_)::value;
@@ -451,35 +471,195 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[FF - 1][t][r] = fmaf(s_now[t], part[t][r], acc[FF - 1][t][r]);
-    if constexpr (!GENERAL) {
-      WAIT_DMA(T::LOADS0);  // bias and gate: this many loads were issued after them
+    if constexpr (KIND == PARTIAL) {
+      f32x4* to = reinterpret_cast<f32x4*>(a.partial) + (int64_t)it.index * (TM * TN / 4) + tid;
+#pragma unroll
+      for (int f = 0; f < FF; ++f)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) to[(f * TT + t) * (64 * T::WAVES)] = acc[f][t];
+    } else {
+      if constexpr (!GENERAL) {
+        WAIT_DMA(T::LOADS0);  // bias and gate: this many loads were issued after them
+        asm volatile("" ::: "memory");
+      }
+      put_tile<Out, KIND, GENERAL, TT, FF>(a, acc, mw, nw, columns, lane);
+      WAIT_LDS();  // bias and gate have been read
       asm volatile("" ::: "memory");
     }
-    put_tile<Out, KIND, GENERAL, TT, FF>(a, acc, mw, nw, columns, lane);
-    WAIT_LDS();  // bias and gate have been read
-    asm volatile("" ::: "memory");
     first_operands(buf);  // again: their registers held what is above
   }
   WAIT_DMA(0);  // the loads past the last stage land before the LDS is another workgroup's
 }
 
-template <typename Out, int KIND, bool EXACT, typename T>
-hipError_t launch_tile(const Fp8Args& a, hipStream_t s) {
-  const int64_t tiles = ((int64_t)a.M + T::TM - 1) / T::TM * ((a.N + T::TN - 1) / T::TN);
-  const dim3 grid((unsigned)std::min<int64_t>(tiles, device_cus() * T::OCC)), block(64 * T::WAVES);
-  if (a.whole)
-    hipLaunchKernelGGL((fp8_tile_kernel<Out, KIND, EXACT, false, T>), grid, block, 0, s, a);
+// --------------------------------------------------------------- few rows
+
+// A value of the output from its sum.
+template <typename Out, int KIND>
+__device__ __forceinline__ void put_one(const Fp8Args& a, float y, int64_t m, int n) {
+  if (a.bias) y += a.bias[n];
+  if constexpr (KIND == ACID_EPI_BIAS_GELU) y = std::is_same_v<Out, bf16> ? gelu_tanh_fast(y) : gelu_tanh(y);
+  if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) y = fmaf(a.gate[n], y, a.residual[m * a.residual_ld + n]);
+  ((Out*)a.out)[m * a.out_ld + n] = (Out)y;
+}
+
+// Up to 16 rows, bound by reading the weights once.  A workgroup has 16 outputs; its WAVES
+// waves take the blocks of inputs in turn, and their sums are added in wave order.  A wave's
+// operands go by way of a part of LDS that is its own: whole lines, DEEP blocks ahead,
+// laid out as the tiles' above.  X: eights of rows.
+template <typename Out, int KIND, bool EXACT, int WAVES, int DEEP, int X>
+__global__ __launch_bounds__(64 * WAVES) void fp8_rows_kernel(Fp8Args a) {
+  constexpr int BLOCK = 2048 + X * 1024 + 128, LOADS = 2 + X + 1;
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[WAVES * DEEP * BLOCK];
+  static_assert(sizeof(ring) >= WAVES * 1024 && sizeof(ring) <= 160 * 1024 && LOADS * (DEEP - 1) <= 63, "ring");
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lg = lane >> 4;
+  const int n0 = blockIdx.x * 16, tail = a.K % kFp8Group;
+  const uint32_t mine = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)ring) + wave * (DEEP * BLOCK);
+  const int row = lane >> 3, chunk = ((lane & 7) ^ lg) * 16;
+  const uint8_t* from[2 + X];  // rows `row` of the eights, outputs first
+#pragma unroll
+  for (int i = 0; i < 2; ++i) from[i] = a.w + (int64_t)std::min(n0 + 8 * i + row, a.N - 1) * a.K;
+#pragma unroll
+  for (int i = 0; i < X; ++i) from[2 + i] = a.a + (int64_t)std::min(8 * i + row, a.M - 1) * a.a_ld;
+  const float* sw = a.w_scales + (int64_t)(n0 / kFp8Group) * a.groups;
+  const float* sx = a.a_scales + std::min(4 * (lane & 3), (a.M - 1) & ~3);
+  auto load = [&](int b, uint32_t at) {
+#pragma unroll
+    for (int i = 0; i < 2 + X; ++i) {
+      const int k = chunk ^ (64 * (i & 1));  // rows 8 i ..: chunk c at slot c ^ (4 i + row / 2) % 8
+      const bool in = !tail || b + 1 < a.groups || k < tail;
+      dma16_from(in ? from[i] + (int64_t)b * kFp8Group + k : reinterpret_cast<const uint8_t*>(&kZeros), at + i * 1024);
+    }
+    if (lane < 4) dma16_from(sx + b * a.a_scales_ld, at + (2 + X) * 1024);
+  };
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  const uint32_t swz = (uint32_t)((lg ^ (lr >> 1)) * 16);
+#pragma unroll
+  for (int i = 0; i < DEEP; ++i)
+    if (wave + i * WAVES < a.groups) load(wave + i * WAVES, mine + i * BLOCK);
+  uint32_t at = mine;
+  for (int b = wave; b < a.groups; b += WAVES) {
+    const float s_out = *(__attribute__((address_space(4))) const float*)uniform_ptr(sw + b);
+    if (b + (DEEP - 1) * WAVES < a.groups) WAIT_DMA(LOADS * (DEEP - 1));
+    else WAIT_DMA(0);
+    asm volatile("" ::: "memory");
+    const uint32_t w_at = at + lr * kFp8Group + swz, x_at = at + 2048 + lr % (8 * X) * kFp8Group + swz;
+    const Pair w = {{lds16(w_at), lds16(w_at ^ 64)}}, x = {{lds16(x_at), lds16(x_at ^ 64)}};
+    const float s = lds4(at + (2 + X) * 1024 + lr * 4) * s_out;
+    WAIT_LDS();
+    asm volatile("" ::: "memory");
+    if (b + DEEP * WAVES < a.groups) load(b + DEEP * WAVES, at);
+    at = at + BLOCK == mine + DEEP * BLOCK ? mine : at + BLOCK;
+    f32x4 part = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        bf16x8 bw[2], bx[2];
+        to_bf16(w.v[j], bw);
+        to_bf16(x.v[j], bx);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[h], bx[h], part, 0, 0, 0);
+      }
+    } else {
+      part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+          __builtin_bit_cast(i32x8, w), __builtin_bit_cast(i32x8, x), part, 0, 0, 0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) acc[r] = fmaf(s, part[r], acc[r]);
+  }
+  __syncthreads();  // (every load has landed)
+  float* sums = reinterpret_cast<float*>(ring);  // [wave][token][output]
+  *reinterpret_cast<f32x4*>(sums + wave * 256 + lr * 16 + 4 * lg) = acc;
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.M * 16; i += 64 * WAVES) {
+    const int n = n0 + i % 16;
+    if (n >= a.N) continue;
+    float y = 0.f;
+#pragma unroll
+    for (int v = 0; v < WAVES; ++v) y += sums[v * 256 + i];
+    put_one<Out, KIND>(a, y, i / 16, n);
+  }
+}
+
+template <typename Out, int KIND, bool EXACT>
+hipError_t launch_rows(const Fp8Args& a, hipStream_t s) {
+  constexpr int WAVES = 8, DEEP = 2;
+  const dim3 grid((a.N + 15) / 16), block(64 * WAVES);
+  if (a.M <= 8)
+    hipLaunchKernelGGL((fp8_rows_kernel<Out, KIND, EXACT, WAVES, DEEP, 1>), grid, block, 0, s, a);
   else
+    hipLaunchKernelGGL((fp8_rows_kernel<Out, KIND, EXACT, WAVES, DEEP, 2>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+// The parts' sums of a split tile, added in order, then its outputs: four a thread.
+template <typename Out, int KIND, typename T>
+__global__ __launch_bounds__(256) void fp8_reduce_kernel(Fp8Args a) {
+  constexpr int EACH = T::TM * T::TN / 4, THREADS = 64 * T::WAVES;
+  const int tiles_n = (a.N + T::TN - 1) / T::TN;
+  const uint32_t tiles_m = (a.M + T::TM - 1) / T::TM, tiles = tiles_m * tiles_n;
+  const uint32_t tile = blockIdx.x / (EACH / 256);
+  const int e = blockIdx.x % (EACH / 256) * 256 + threadIdx.x;
+  int64_t tm;
+  int tn;
+  tile_coords<4>(tile, tiles_m, tiles_n, tm, tn);
+  const int q = e / THREADS, wave = e % THREADS / 64, lane = e % 64;
+  const int64_t m = tm * T::TM + (wave % T::WT * T::TT + q % T::TT) * 16 + (lane & 15);
+  const int n = tn * T::TN + (wave / T::WT * T::FF + q / T::TT) * 16 + 4 * (lane >> 4);
+  if (m >= a.M || n >= a.N) return;
+  const f32x4* from = reinterpret_cast<const f32x4*>(a.partial) + (int64_t)tile * EACH + e;
+  f32x4 y = from[0];
+  for (int s = 1; s < a.split; s += 4) {  // four in flight; past the last: read again and dropped
+    f32x4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = from[(int64_t)std::min(s + j, a.split - 1) * tiles * EACH];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (s + j < a.split) y += v[j];
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (n + r < a.N) put_one<Out, KIND>(a, y[r], m, n + r);
+}
+
+template <typename Out, int KIND, bool EXACT, typename T>
+hipError_t launch_tile(Fp8Args a, int split, hipStream_t s) {
+  a.split = split;
+  const int64_t tiles = ((int64_t)a.M + T::TM - 1) / T::TM * ((a.N + T::TN - 1) / T::TN);
+  const dim3 grid((unsigned)std::min<int64_t>(tiles * split, device_cus() * T::OCC)), block(64 * T::WAVES);
+  if constexpr (T::TM < 256) {
+    if (split > 1) {
+      if (a.K % kFp8Group == 0)
+        hipLaunchKernelGGL((fp8_tile_kernel<float, PARTIAL, EXACT, false, T>), grid, block, 0, s, a);
+      else
+        hipLaunchKernelGGL((fp8_tile_kernel<float, PARTIAL, EXACT, true, T>), grid, block, 0, s, a);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((fp8_reduce_kernel<Out, KIND, T>), dim3((unsigned)(tiles * (T::TM * T::TN / 1024))), dim3(256), 0, s, a);
+      return hipGetLastError();
+    }
+  }
+  if (a.whole) {
+    hipLaunchKernelGGL((fp8_tile_kernel<Out, KIND, EXACT, false, T>), grid, block, 0, s, a);
+  } else {
     hipLaunchKernelGGL((fp8_tile_kernel<Out, KIND, EXACT, true, T>), grid, block, 0, s, a);
+  }
   return hipGetLastError();
 }
 
 template <typename Out, int KIND, bool EXACT>
 hipError_t launch(const Fp8Args& a, hipStream_t s) {
-  if constexpr (EXACT)
-    return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, 4, 1>>(a, s);
-  else
-    return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, 8, 1>>(a, s);
+  const Fp8Form f = fp8_form(a.M, a.N, a.K, EXACT, device_cus());
+  switch (f.tile) {
+    case Fp8Tile::kRows: return launch_rows<Out, KIND, EXACT>(a, s);
+    case Fp8Tile::k64: return launch_tile<Out, KIND, EXACT, Tile<4, 1, 1, 4, 4>>(a, f.split, s);
+    case Fp8Tile::k128: return launch_tile<Out, KIND, EXACT, Tile<2, 2, 4, 4, 2>>(a, f.split, s);
+    case Fp8Tile::k256: break;
+  }
+  // (exact products hold their tokens' operands twice: 256 x 128)
+  return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, EXACT ? 4 : 8, 1>>(a, 1, s);
 }
 
 }  // namespace
@@ -490,10 +670,9 @@ using namespace acid;
 extern "C" {
 
 size_t acid_linear_fp8_workspace_needed(int64_t M, int32_t N, int32_t K) {
-  (void)M;
-  (void)N;
-  (void)K;
-  return 0;
+  if (M < 1 || N < 1 || K < 1 || K % 16 || M > (1 << 24) || N > (1 << 22) || K > (1 << 22)) return 0;
+  const int64_t cus = device_cus();
+  return sizeof(float) * (size_t)std::max(fp8_form(M, N, K, false, cus).floats, fp8_form(M, N, K, true, cus).floats);
 }
 
 acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t N, int32_t K,
@@ -557,8 +736,8 @@ acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t
                      (uintptr_t)p.bias % 16 == 0 &&
                      (!update || (p.residual_ld % 4 == 0 && ((uintptr_t)p.residual | (uintptr_t)p.gate) % 16 == 0));
   const Fp8Args a = {(const uint8_t*)p.a, (const uint8_t*)p.w, p.a_scales, p.w_scales, p.bias, p.gate,
-                     p.residual, p.out, p.a_ld, p.a_scales_ld, p.residual_ld, p.out_ld, (int32_t)M, N,
-                     K, (int32_t)groups, whole};
+                     p.residual, p.out, p.a_ld, p.a_scales_ld, p.residual_ld, p.out_ld, (float*)p.workspace, (int32_t)M, N,
+                     K, (int32_t)groups, 1, whole};
   hipError_t e;
   if (p.out_dtype == ACID_BF16)
     e = p.kind == ACID_EPI_BIAS ? launch<bf16, ACID_EPI_BIAS, false>(a, stream)
