@@ -25,7 +25,7 @@ struct HeadArgs {
   const float *q_weight, *k_weight, *q_bias, *k_bias;
   int64_t tokens, tiles, v_tiles, qk_groups;  // of a sequence; workgroups of Q and K
   int32_t heads, kv_heads, pairs, ends[3];  // ends of the first three axes' pairs
-  int32_t norm, halves, float_positions;
+  int32_t norm, halves, float_positions, vt_wide;
   float q_scale, eps;
 };
 
@@ -56,39 +56,66 @@ __device__ __forceinline__ void store8(float* p, const float* v) {
   *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 
+// Sixteen values of a head as they were loaded: two runs of eight.
+template <typename T>
+struct Held;
+template <>
+struct Held<bf16> {
+  u32x4 v[2];
+  __device__ __forceinline__ void load(const bf16* p, int d0, int d1) {
+    v[0] = *reinterpret_cast<const u32x4*>(p + d0);
+    v[1] = *reinterpret_cast<const u32x4*>(p + d1);
+  }
+  __device__ __forceinline__ void values(float* x) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[2 * i] = __uint_as_float(v[i / 4][i % 4] << 16);
+      x[2 * i + 1] = __uint_as_float(v[i / 4][i % 4] & 0xffff0000u);
+    }
+  }
+};
+template <>
+struct Held<float> {
+  f32x4 v[4];
+  __device__ __forceinline__ void load(const float* p, int d0, int d1) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      v[i] = *reinterpret_cast<const f32x4*>(p + d0 + 4 * i);
+      v[2 + i] = *reinterpret_cast<const f32x4*>(p + d1 + 4 * i);
+    }
+  }
+  __device__ __forceinline__ void values(float* x) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = v[i / 4][i % 4];
+  }
+};
+
 // Sum over the lanes that hold one head of a token.
 template <int LANES>
 __device__ __forceinline__ float head_sum(float v) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+#define ADD_DPP(ctrl) \
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), ctrl, 0xf, 0xf, false))
+  ADD_DPP(0xB1);                             // the lane beside it
+  ADD_DPP(0x4E);                             // the other two of its four
+  if constexpr (LANES == 8) ADD_DPP(0x141);  // the other four of its eight
+#undef ADD_DPP
   return v;
 }
 
-// Q and K of 64 / (D / 16) tokens: a lane holds sixteen values of a head, eight
-// pairs, and the four waves take the heads in turn.  The angles' sines and cosines
-// are made once and shared by way of LDS.
+// Q and K of 64 / (D / 16) tokens: a lane holds sixteen values of a head, eight pairs, and
+// the eight waves take the heads in turn.  Up to HELD heads a wave are loaded at once and
+// stay in registers between their norm's sum and their rotation (more of them are read
+// again: 32 heads of Q and K together are 8 x HELD).  The angles' sines and cosines are made once a
+// token and shared by way of LDS, while the heads are on their way.
+constexpr int kWaves = 8, HELD = 4;
 template <typename In, typename Out, int D>
 __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, float* lds) {
   constexpr int LANES = D / 16, TOKENS = 64 / LANES;
-  float2* turns = reinterpret_cast<float2*>(lds);                  // [TOKENS][D / 2]
-  float* part = lds + TOKENS * D;                                  // [2][4][TOKENS]
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float2* turns = reinterpret_cast<float2*>(lds);  // [TOKENS][D / 2]
+  float* part = lds + TOKENS * D;                  // [2][kWaves][TOKENS]
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t seq = group / a.tiles, t0 = (group - seq * a.tiles) * TOKENS;
-  for (int i = tid; i < TOKENS * (D / 2); i += 256) {
-    const int p = i % (D / 2);
-    const int64_t t = t0 + i / (D / 2);
-    float2 cs = make_float2(1.f, 0.f);
-    if (p < a.pairs && t < a.tokens) {
-      const int axis = (p >= a.ends[0]) + (p >= a.ends[1]) + (p >= a.ends[2]);
-      const int64_t at = axis * a.positions_ld + seq * a.tokens + t;
-      const double pos = a.float_positions ? (double)((const float*)a.positions)[at]
-                                           : (double)((const int32_t*)a.positions)[at];
-      double turn = pos * (a.freqs[p] * 0.15915494309189535);  // 1 / (2 pi)
-      turn -= rint(turn);
-      sincospif(2.0f * (float)turn, &cs.y, &cs.x);
-    }
-    turns[i] = cs;
-  }
   const int o = lane % LANES, tt = lane / LANES;
   const int64_t t = t0 + tt < a.tokens ? t0 + tt : a.tokens - 1, row = seq * a.tokens + t;
   const bool live = t0 + tt < a.tokens;
@@ -98,24 +125,52 @@ __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, f
     d0 = 8 * o;
     d1 = a.pairs + d0;
   }
-  const int nq = a.q ? a.heads : 0, nk = a.k ? a.kv_heads : 0;
+  const int nq = a.q ? a.heads : 0, nk = a.k ? a.kv_heads : 0, n = nq + nk;
+  auto source = [&](int u) {
+    return u < nq ? (const In*)a.q + row * a.q_ld + u * D : (const In*)a.k + row * a.k_ld + (u - nq) * D;
+  };
+  Held<In> held[HELD];
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (wave + kWaves * i < n) held[i].load(source(wave + kWaves * i), d0, d1);
+
+  for (int i = tid; i < TOKENS * (D / 2); i += 64 * kWaves) {
+    const int p = i % (D / 2);
+    const int64_t ti = t0 + i / (D / 2);
+    float2 cs = make_float2(1.f, 0.f);
+    if (p < a.pairs && ti < a.tokens) {
+      const int axis = (p >= a.ends[0]) + (p >= a.ends[1]) + (p >= a.ends[2]);
+      const int64_t at = axis * a.positions_ld + seq * a.tokens + ti;
+      const double pos = a.float_positions ? (double)((const float*)a.positions)[at]
+                                           : (double)((const int32_t*)a.positions)[at];
+      double turn = pos * (a.freqs[p] * 0.15915494309189535);  // 1 / (2 pi)
+      turn -= rint(turn);
+      sincospif(2.0f * (float)turn, &cs.y, &cs.x);
+    }
+    turns[i] = cs;
+  }
   if (a.norm == ACID_HEAD_NORM_RMS_ROW) {
     float sums[2] = {0.f, 0.f};
-    for (int u = wave; u < nq + nk; u += 4) {
-      const bool is_q = u < nq;
-      const In* src = is_q ? (const In*)a.q + row * a.q_ld + u * D : (const In*)a.k + row * a.k_ld + (u - nq) * D;
+    auto add = [&](const Held<In>& h, int u) {
       float v[16], s = 0.f;
-      load8(src + d0, v);
-      load8(src + d1, v + 8);
+      h.values(v);
 #pragma unroll
       for (int i = 0; i < 16; ++i) s = fmaf(v[i], v[i], s);
-      if (is_q) sums[0] += s;
-      else sums[1] += s;
+      sums[0] += u < nq ? s : 0.f;
+      sums[1] += u < nq ? 0.f : s;
+    };
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (wave + kWaves * i < n) add(held[i], wave + kWaves * i);
+    for (int u = wave + kWaves * HELD; u < n; u += kWaves) {
+      Held<In> h;
+      h.load(source(u), d0, d1);
+      add(h, u);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float s = head_sum<LANES>(sums[i]);
-      if (o == 0) part[(i * 4 + wave) * TOKENS + tt] = s;
+      if (o == 0) part[(i * kWaves + wave) * TOKENS + tt] = s;
     }
   }
   __syncthreads();
@@ -123,67 +178,67 @@ __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, f
   if (a.norm == ACID_HEAD_NORM_RMS_ROW) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float* p = part + i * 4 * TOKENS + tt;
-      const float s = (p[0] + p[TOKENS]) + (p[2 * TOKENS] + p[3 * TOKENS]);
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) s += part[(i * kWaves + w) * TOKENS + tt];
       row_r[i] = 1.0f / sqrtf(s / (float)((i ? a.kv_heads : a.heads) * D) + a.eps);
     }
   }
   float2 cs[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) cs[i] = turns[tt * (D / 2) + 8 * o + i];
-  for (int u = wave; u < nq + nk; u += 4) {
+
+  auto finish = [&](const Held<In>& h, int u) {
     const bool is_q = u < nq;
     const int head = is_q ? u : u - nq;
-    const In* src = is_q ? (const In*)a.q + row * a.q_ld + head * D : (const In*)a.k + row * a.k_ld + head * D;
     float v[16];
-    load8(src + d0, v);
-    load8(src + d1, v + 8);
+    h.values(v);
     if (a.norm != ACID_HEAD_NORM_NONE) {
-      float mean = 0.f, r = is_q ? row_r[0] : row_r[1];
+      float r = is_q ? row_r[0] : row_r[1];
       const float* weight = is_q ? a.q_weight : a.k_weight;
       const float* bias = is_q ? a.q_bias : a.k_bias;
-      if (a.norm == ACID_HEAD_NORM_LAYER) {
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s += v[i];
-        mean = head_sum<LANES>(s) / D;
-      }
-      if (a.norm != ACID_HEAD_NORM_RMS_ROW) {
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          v[i] -= mean;
-          s = fmaf(v[i], v[i], s);
-        }
-        r = 1.0f / sqrtf(head_sum<LANES>(s) / D + a.eps);
-      } else if (weight) {
-        weight += head * D;
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int dim = i < 8 ? d0 + i : d1 + i - 8;
-        v[i] *= r;
-        if (weight) v[i] *= weight[dim];
-        if (bias) v[i] += bias[dim];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool turned = 8 * o + i < a.pairs;
-      const float vx = a.halves ? v[i] : v[2 * i], vy = a.halves ? v[8 + i] : v[2 * i + 1];
-      const float nx = turned ? vx * cs[i].x - vy * cs[i].y : vx;
-      const float ny = turned ? vx * cs[i].y + vy * cs[i].x : vy;
-      if (a.halves) {
-        v[i] = nx;
-        v[8 + i] = ny;
+      if (a.norm == ACID_HEAD_NORM_RMS_ROW) {
+        if (weight) weight += head * D;
       } else {
-        v[2 * i] = nx;
-        v[2 * i + 1] = ny;
-      }
-    }
-    if (is_q) {
+        if (a.norm == ACID_HEAD_NORM_LAYER) {
+          float s = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] *= a.q_scale;
+          for (int i = 0; i < 16; ++i) s += v[i];
+          const float mean = head_sum<LANES>(s) / D;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] -= mean;
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s = fmaf(v[i], v[i], s);
+        r = 1.0f / sqrtf(head_sum<LANES>(s) / D + a.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] *= r;
+      auto each = [&](const float* p, auto f) {  // f(value, the column's)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 w = *reinterpret_cast<const f32x4*>(p + (j < 2 ? d0 : d1 - 8) + 4 * j);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[4 * j + i] = f(v[4 * j + i], w[i]);
+        }
+      };
+      if (weight) each(weight, [](float x, float w) { return x * w; });
+      if (bias) each(bias, [](float x, float b) { return x + b; });
+    }
+    const float scale = is_q ? a.q_scale : 1.f;
+    auto turn = [&](float& x, float& y, int i) {
+      const bool turned = 8 * o + i < a.pairs;
+      const float nx = x * cs[i].x - y * cs[i].y, ny = x * cs[i].y + y * cs[i].x;
+      x = scale * (turned ? nx : x);
+      y = scale * (turned ? ny : y);
+    };
+    if (a.halves) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) turn(v[i], v[8 + i], i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) turn(v[2 * i], v[2 * i + 1], i);
     }
     if (live) {
       Out* dst = is_q ? (Out*)a.q_out + seq * a.q_seq + head * a.q_head + t * a.q_row
@@ -191,41 +246,53 @@ __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, f
       store8(dst + d0, v);
       store8(dst + d1, v + 8);
     }
+  };
+#pragma unroll
+  for (int i = 0; i < HELD; ++i)
+    if (wave + kWaves * i < n) finish(held[i], wave + kWaves * i);
+  for (int u = wave + kWaves * HELD; u < n; u += kWaves) {
+    Held<In> h;
+    h.load(source(u), d0, d1);
+    finish(h, u);
   }
 }
 
-// V^T of 64 tokens and 64 dims of a head, by way of LDS.
+// V^T of 64 tokens and 64 dims of a head, by way of LDS: eight dims of a token a thread
+// in, eight tokens of a dim out.
 template <typename In, typename Out, int D>
 __device__ __forceinline__ void transpose_v(const HeadArgs& a, int64_t group, float* lds) {
-  constexpr int PITCH = 65;
-  const int tid = threadIdx.x;
-  const int64_t per_seq = a.v_tiles * a.kv_heads * (D / 64);
-  const int64_t seq = group / per_seq;
-  const int64_t rest = group - seq * per_seq;
-  const int part = (int)(rest % (a.kv_heads * (D / 64)));
-  const int64_t t0 = rest / (a.kv_heads * (D / 64)) * 64;
+  constexpr int PITCH = 64 + 16 / sizeof(Out);  // of a dim's tokens
+  Out* tile = reinterpret_cast<Out*>(lds);
+  const int tid = threadIdx.x, units = a.kv_heads * (D / 64);
+  const int64_t per_seq = a.v_tiles * units, seq = group / per_seq, rest = group - seq * per_seq;
+  const int part = (int)(rest % units);
+  const int64_t t0 = rest / units * 64;
   const int head = part / (D / 64), dim0 = part % (D / 64) * 64;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int at = tid + 256 * i, r = at / 8, c = at % 8 * 8;
-    const int64_t t = t0 + r < a.tokens ? t0 + r : a.tokens - 1;
+  const int left = (int)(a.tokens - t0 < 64 ? a.tokens - t0 : 64);
+  {
+    const int r = tid / 8, c = tid % 8 * 8;
     float v[8];
-    load8((const In*)a.v + (seq * a.tokens + t) * a.v_ld + head * D + dim0 + c, v);
+    load8((const In*)a.v + (seq * a.tokens + t0 + (r < left ? r : left - 1)) * a.v_ld + head * D + dim0 + c, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) lds[r * PITCH + c + e] = v[e];
+    for (int e = 0; e < 8; ++e) tile[(c + e) * PITCH + r] = (Out)v[e];
   }
   __syncthreads();
-  Out* vt = (Out*)a.vt + seq * a.vt_seq + head * a.vt_head + dim0 * a.vt_row + t0;
-  const int left = (int)(a.tokens - t0 < 64 ? a.tokens - t0 : 64);
-  for (int i = tid; i < 64 * 64; i += 256) {
-    const int dim = i / 64, t = i % 64;
-    if (t < left) vt[dim * a.vt_row + t] = (Out)lds[t * PITCH + dim];
+  const int dim = tid / 8, c = tid % 8 * 8;
+  const Out* from = tile + dim * PITCH + c;
+  Out* to = (Out*)a.vt + seq * a.vt_seq + head * a.vt_head + (dim0 + dim) * a.vt_row + t0 + c;
+  if (a.vt_wide && c + 8 <= left) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(Out) / 2; ++i)
+      reinterpret_cast<u32x4*>(to)[i] = reinterpret_cast<const u32x4*>(from)[i];
+  } else {
+    for (int e = 0; e < 8 && c + e < left; ++e) to[e] = from[e];
   }
 }
 
 template <typename In, typename Out, int D>
-__global__ __launch_bounds__(256) void rotary_qkv_kernel(HeadArgs a) {
-  __shared__ float lds[64 * 65];
+__global__ __launch_bounds__(64 * kWaves) void rotary_qkv_kernel(HeadArgs a) {
+  constexpr int TURNS = 1024 / D * D + 2 * kWaves * (1024 / D), TILE = 64 * (64 + 16 / sizeof(Out)) * sizeof(Out) / 4;
+  __shared__ __attribute__((aligned(16))) float lds[TURNS > TILE ? TURNS : TILE];
   if ((int64_t)blockIdx.x < a.qk_groups)
     rotate_heads<In, Out, D>(a, blockIdx.x, lds);
   else
@@ -235,9 +302,9 @@ __global__ __launch_bounds__(256) void rotary_qkv_kernel(HeadArgs a) {
 template <typename In, typename Out>
 hipError_t launch(int d, const HeadArgs& a, unsigned grid, hipStream_t s) {
   if (d == 64)
-    hipLaunchKernelGGL((rotary_qkv_kernel<In, Out, 64>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((rotary_qkv_kernel<In, Out, 64>), dim3(grid), dim3(64 * kWaves), 0, s, a);
   else
-    hipLaunchKernelGGL((rotary_qkv_kernel<In, Out, 128>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((rotary_qkv_kernel<In, Out, 128>), dim3(grid), dim3(64 * kWaves), 0, s, a);
   return hipGetLastError();
 }
 
@@ -380,14 +447,16 @@ acid_status acid_rotary_qkv(const acid_rotary_qkv_args* args, int64_t n_seq, int
   }
   const int64_t tile = 1024 / d, tiles = (tokens + tile - 1) / tile, v_tiles = (tokens + 63) / 64;
   const int64_t qk = p.q || p.k ? n_seq * tiles : 0, vg = p.v ? n_seq * v_tiles * p.kv_heads * (d / 64) : 0;
-  if (qk + vg >= (1 << 24))
-    return set_error(ACID_ERR_SHAPE, "rotary: sequences, tokens and heads need %lld workgroups, at most 2^24 - 1",
+  if (qk + vg >= (1 << 23))
+    return set_error(ACID_ERR_SHAPE, "rotary: sequences, tokens and heads need %lld workgroups, at most 2^23 - 1",
                      (long long)(qk + vg));
+  const int32_t vt_wide = ((uintptr_t)p.vt | (uintptr_t)(p.vt_row * os) | (uintptr_t)(p.vt_head * os) |
+                           (uintptr_t)(p.vt_seq * os)) % 16 == 0;
   HeadArgs a = {p.q, p.k, p.v, p.q_out, p.k_out, p.vt, p.q_ld, p.k_ld, p.v_ld,
                 p.q_head, p.q_row, p.q_seq, p.k_head, p.k_row, p.k_seq, p.vt_head, p.vt_row, p.vt_seq,
                 p.positions, p.positions_ld, p.freqs, p.q_weight, p.k_weight, p.q_bias, p.k_bias,
                 tokens, tiles, v_tiles, qk, p.heads, p.kv_heads, pairs, {ends[0], ends[1], ends[2]},
-                p.norm, p.pairing, p.positions_f32, p.q_scale, p.eps};
+                p.norm, p.pairing, p.positions_f32, vt_wide, p.q_scale, p.eps};
   StreamDevice on;
   ACID_TRY(on.enter(stream));
   const unsigned grid = (unsigned)(qk + vg);
