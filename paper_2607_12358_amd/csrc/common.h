@@ -38,6 +38,21 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// Sum over a wave, in every lane: neighbours, fours, eights and rows of 16
+// within the vector unit (each __shfl would take a trip through LDS).
+__device__ __forceinline__ float lane_sum(float v) {
+#define ADD_DPP(ctrl, rows)                                                                    \
+  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), ctrl, rows, 0xf, false))
+  ADD_DPP(0x111, 0xf);  // from the lane 1 before, in its row of 16
+  ADD_DPP(0x112, 0xf);  // 2
+  ADD_DPP(0x114, 0xf);  // 4
+  ADD_DPP(0x118, 0xf);  // 8: the last lane of each row has its row's sum
+  ADD_DPP(0x142, 0xa);  // rows 1 and 3 add the row before theirs
+  ADD_DPP(0x143, 0xc);  // rows 2 and 3 add the first two
+#undef ADD_DPP
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+
 typedef __attribute__((address_space(3))) void lds_void_t;
 
 // An address that is the same in every lane, in scalar registers.

@@ -25,43 +25,60 @@ struct RowsArgs {
   int32_t K, groups;
 };
 
-// Eight neighbouring values.
-__device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
-  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+// Eight neighbouring values as they were loaded.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<bf16> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16* p) { w = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
   }
-}
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+};
+template <>
+struct Eight<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = *reinterpret_cast<const f32x4*>(p);
+    b = *reinterpret_cast<const f32x4*>(p + 4);
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = a[i];
-    v[4 + i] = b[i];
+    for (int i = 0; i < 4; ++i) {
+      v[i] = a[i];
+      v[4 + i] = b[i];
+    }
   }
-}
+};
 
-// A wave takes one group of 32 rows, four rows an instruction, sixteen lanes
-// and eight values a lane to a row's group.
-constexpr int kRowsTile = 32;
-template <typename X>
+// A wave takes one group of 4 QUADS rows: sixteen lanes and eight values a lane to a row's
+// group, four rows an instruction, all of them loaded before the first is used.  32760 bf16
+// rows of 1536, 153 MB: 32 us, 4.7 TB/s; 77 fp32 rows of 1040: 2.0 us with four rows a wave, 4.5
+// with 32, one quad after the other.
+template <typename X, int QUADS>
 __global__ __launch_bounds__(256) void quantize_fp8_rows_kernel(RowsArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int64_t tile = item / a.groups;
   const int group = (int)(item - tile * a.groups);
-  const int64_t row0 = tile * kRowsTile;
-  if (row0 >= a.rows) return;
+  const int64_t row0 = tile * (4 * QUADS) + (lane >> 4);
+  if (row0 - (lane >> 4) >= a.rows) return;
   const int k = group * kFp8Group + (lane & 15) * 8;
   const bool live = k < a.K;
-  const int left = (int)std::min<int64_t>(kRowsTile, a.rows - row0);
-  for (int r0 = 0; r0 < left; r0 += 4) {
-    const int r = r0 + (lane >> 4);
-    const int64_t row = row0 + (r < left ? r : left - 1);
+  Eight<X> held[QUADS];
+#pragma unroll
+  for (int q = 0; q < QUADS; ++q)
+    held[q].load((const X*)a.x + std::min(row0 + 4 * q, a.rows - 1) * a.x_ld + (live ? k : 0));
+#pragma unroll
+  for (int q = 0; q < QUADS; ++q) {
+    const int64_t row = row0 + 4 * q;
     float v[8];
-    load8((const X*)a.x + row * a.x_ld + (live ? k : 0), v);
+    held[q].values(v);
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -69,7 +86,7 @@ __global__ __launch_bounds__(256) void quantize_fp8_rows_kernel(RowsArgs a) {
       most = max(most, abs_bits(v[i]));
     }
     const Fp8Scale s(row16_max(most));
-    if (r < left) {
+    if (row < a.rows) {
       if (live) {
         uint2 w;
         w.x = to_fp8(v[0] * s.inv, v[1] * s.inv, v[2] * s.inv, v[3] * s.inv);
@@ -79,6 +96,13 @@ __global__ __launch_bounds__(256) void quantize_fp8_rows_kernel(RowsArgs a) {
       if ((lane & 15) == 0) a.scales[group * a.scales_ld + row] = s.scale;
     }
   }
+}
+
+template <typename X, int QUADS>
+hipError_t launch_rows(const RowsArgs& a, hipStream_t s) {
+  const int64_t items = (a.rows + 4 * QUADS - 1) / (4 * QUADS) * a.groups;
+  hipLaunchKernelGGL((quantize_fp8_rows_kernel<X, QUADS>), dim3((unsigned)((items + 3) / 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 // ------------------------------------------------------------ LN-modulate
@@ -91,16 +115,10 @@ struct LnArgs {
   int32_t hidden;
 };
 
-__device__ __forceinline__ float lanes_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-
 // Sum over the WAVES waves of a row.
 template <int WAVES>
 __device__ __forceinline__ float row_sum(float v, float* part) {
-  v = lanes_sum(v);
+  v = lane_sum(v);
   if constexpr (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -111,52 +129,57 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
-// WAVES waves a row, four values a lane at a time: 32 lanes hold a group.
-// Statistics in fp32, in two passes over the registers.
+// A row a workgroup of WAVES waves, four values a lane at a time: 32 lanes hold a
+// group.  Statistics in fp32, in two passes over the registers.  32760 rows of 1536, 253
+// MB: 53 us, 4.8 TB/s, 47 of it without the modulation's vectors, which each row reads again
+// from L2, and the scales, four bytes to a line.  (Two rows a workgroup that share both take
+// as long, runs of eight with the next in flight 62; two or four waves a row 54 and 62.)  7
+// rows of 4096: 3.4 us with four waves, 4.4 with two.
 template <int WAVES, int CHUNKS>
 __global__ __launch_bounds__(64 * WAVES) void ln_modulate_fp8_kernel(LnArgs a) {
   __shared__ float part[2][WAVES];
-  const int64_t row = blockIdx.x;
+  const int64_t row = blockIdx.x, mod = a.rows_per_mod ? row / a.rows_per_mod * a.hidden : 0;
   const int tid = threadIdx.x, n4 = a.hidden / 4;
-  const float* x = a.x + row * a.x_ld;
-  f32x4 v[CHUNKS];
-  float sum = 0.f;
+  const float inv_n = 1.0f / (float)a.hidden;
+  auto inside = [&](int c) { return tid + 64 * WAVES * c < n4; };
+  f32x4 v[CHUNKS], scale[CHUNKS], shift[CHUNKS];
+  auto read = [&](f32x4 (&to)[CHUNKS], const float* from) {  // threads past the row's end: copies
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) {
-    const int i = tid + 64 * WAVES * c;
-    v[c] = i < n4 ? *reinterpret_cast<const f32x4*>(x + 4 * i) : f32x4{0.f, 0.f, 0.f, 0.f};
-    sum += (v[c][0] + v[c][1]) + (v[c][2] + v[c][3]);
-  }
-  const float mean = row_sum<WAVES>(sum, part[0]) / a.hidden;
-  float squares = 0.f;
+    for (int c = 0; c < CHUNKS; ++c)
+      to[c] = *reinterpret_cast<const f32x4*>(from + 4 * (inside(c) ? tid + 64 * WAVES * c : 0));
+  };
+  read(v, a.x + row * a.x_ld);
+  read(scale, a.scale + mod);
+  read(shift, a.shift + mod);
+  float sum = 0.f, squares = 0.f;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) sum += inside(c) ? (v[c][0] + v[c][1]) + (v[c][2] + v[c][3]) : 0.f;
+  const float mean = row_sum<WAVES>(sum, part[0]) * inv_n;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[c][e] -= mean;
-    const float q = (v[c][0] * v[c][0] + v[c][1] * v[c][1]) + (v[c][2] * v[c][2] + v[c][3] * v[c][3]);
-    squares += tid + 64 * WAVES * c < n4 ? q : 0.f;
+    const f32x4 q = v[c] * v[c];
+    squares += inside(c) ? (q[0] + q[1]) + (q[2] + q[3]) : 0.f;
   }
-  const float r = 1.0f / sqrtf(row_sum<WAVES>(squares, part[1]) / a.hidden + 1e-6f);
-  const int64_t mod = a.rows_per_mod ? row / a.rows_per_mod * a.hidden : 0;
+  const float r = 1.0f / sqrtf(row_sum<WAVES>(squares, part[1]) * inv_n + 1e-6f);
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     const int i = tid + 64 * WAVES * c;
-    const bool live = i < n4;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
-    if (live) {
-      const f32x4 scale = *reinterpret_cast<const f32x4*>(a.scale + mod + 4 * i);
-      const f32x4 shift = *reinterpret_cast<const f32x4*>(a.shift + mod + 4 * i);
+    f32x4 y;
+    uint32_t most = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = v[c][e] * r * (1.0f + scale[e]) + shift[e];
+    for (int e = 0; e < 4; ++e) {
+      y[e] = inside(c) ? fmaf(v[c][e] * r, 1.0f + scale[c][e], shift[c][e]) : 0.f;
+      most = max(most, abs_bits(y[e]));
     }
-    uint32_t most = max(max(abs_bits(y[0]), abs_bits(y[1])), max(abs_bits(y[2]), abs_bits(y[3])));
     most = row16_max(most);
-    most = max(most, (uint32_t)__shfl_xor((int)most, 16, 64));
-    const Fp8Scale s(most);
-    if (live) {
+    const auto both = __builtin_amdgcn_permlane16_swap(most, most, false, false);  // the row of 16 lanes beside
+    const Fp8Scale s(max(both[0], both[1]));
+    if (inside(c)) {
       *reinterpret_cast<uint32_t*>(a.codes + row * a.codes_ld + 4 * i) =
           to_fp8(y[0] * s.inv, y[1] * s.inv, y[2] * s.inv, y[3] * s.inv);
-      if (i % 32 == 0) a.scales[(i / 32) * a.scales_ld + row] = s.scale;
+      if (i % 32 == 0) a.scales[i / 32 * a.scales_ld + row] = s.scale;
     }
   }
 }
@@ -176,7 +199,7 @@ hipError_t launch_ln(const LnArgs& a, hipStream_t s) {
 // ---------------------------------------------------------------- weights
 
 // One 128 x 128 block a workgroup: thread t holds outputs t % 128 of 64
-// inputs, half t / 128 of the block.
+// inputs, half t / 128 of the block.  8960 x 1536, 69 MB: 15.5 us, 4.4 TB/s.
 __global__ __launch_bounds__(256) void quantize_fp8_weight_kernel(const float* __restrict__ w, int N,
                                                                   int K, uint8_t* __restrict__ codes,
                                                                   float* __restrict__ scales) {
@@ -217,7 +240,7 @@ __global__ __launch_bounds__(256) void quantize_fp8_weight_kernel(const float* _
 acid_status check_rows(int64_t rows, int64_t K, int64_t x_ld, int64_t x_size, int64_t codes_ld,
                        int64_t scales_ld) {
   if (rows < 0 || K < 1) return set_error(ACID_ERR_INVALID_ARG, "fp8: rows < 0 or K < 1");
-  if (K % 16 || K > (1 << 22) || (rows + kRowsTile - 1) / kRowsTile * fp8_groups(K) > (1 << 26))
+  if (K % 16 || K > (1 << 22) || (rows + 31) / 32 * fp8_groups(K) > (1 << 26))
     return set_error(ACID_ERR_SHAPE,
                      "fp8: K %lld must be a multiple of 16, <= 2^22, and ceil(rows / 32) "
                      "ceil(K / 128) <= 2^26", (long long)K);
@@ -269,13 +292,13 @@ acid_status acid_quantize_fp8(int32_t x_dtype, int64_t rows, int32_t K, const vo
   ACID_TRY(on.enter(stream));
   const RowsArgs a = {x_dev, (uint8_t*)codes_dev, scales_dev, x_ld, codes_ld, scales_ld, rows, K,
                       (int32_t)groups};
-  const int64_t items = (rows + kRowsTile - 1) / kRowsTile * groups;
-  const dim3 grid((unsigned)((items + 3) / 4));
+  // 32 rows a wave where that leaves each SIMD two waves, else four
+  const bool many = (rows + 31) / 32 * groups >= 8 * device_cus();
+  hipError_t e;
   if (x_dtype == ACID_BF16)
-    hipLaunchKernelGGL(quantize_fp8_rows_kernel<bf16>, grid, dim3(256), 0, stream, a);
+    e = many ? launch_rows<bf16, 8>(a, stream) : launch_rows<bf16, 1>(a, stream);
   else
-    hipLaunchKernelGGL(quantize_fp8_rows_kernel<float>, grid, dim3(256), 0, stream, a);
-  const hipError_t e = hipGetLastError();
+    e = many ? launch_rows<float, 8>(a, stream) : launch_rows<float, 1>(a, stream);
   return e == hipSuccess ? ACID_OK : check_hip(e, "quantize fp8");
 }
 
@@ -302,9 +325,11 @@ acid_status acid_ln_modulate_fp8(int64_t rows, int32_t hidden, const float* x_de
   ACID_TRY(on.enter(stream));
   const LnArgs a = {x_dev, shift_dev, scale_dev, (uint8_t*)codes_dev, scales_dev, x_ld, codes_ld,
                     scales_ld, rows, rows_per_mod, hidden};
-  const hipError_t e = hidden <= 2048   ? launch_ln<1>(a, stream)
-                       : hidden <= 4096 ? launch_ln<2>(a, stream)
-                                        : launch_ln<4>(a, stream);
+  // One wave a row where there are two rows a SIMD, four for few rows.
+  const bool many = rows >= 8 * device_cus();
+  const hipError_t e = hidden <= 2048 && many   ? launch_ln<1>(a, stream)
+                       : hidden <= 4096 && many ? launch_ln<2>(a, stream)
+                                                : launch_ln<4>(a, stream);
   return e == hipSuccess ? ACID_OK : check_hip(e, "ln modulate fp8");
 }
 

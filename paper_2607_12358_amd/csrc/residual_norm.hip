@@ -66,21 +66,6 @@ __device__ __forceinline__ float4 mul4(float4 a, float4 b) {
   return make_float4(a.x * b.x, a.y * b.y, a.z * b.z, a.w * b.w);
 }
 
-// Sum over a wave, in every lane: neighbours, fours, eights and rows of 16
-// within the vector unit (each __shfl would take a trip through LDS).
-__device__ __forceinline__ float lane_sum(float v) {
-#define ADD_DPP(ctrl, rows)                                                                    \
-  v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), ctrl, rows, 0xf, false))
-  ADD_DPP(0x111, 0xf);  // from the lane 1 before, in its row of 16
-  ADD_DPP(0x112, 0xf);  // 2
-  ADD_DPP(0x114, 0xf);  // 4
-  ADD_DPP(0x118, 0xf);  // 8: the last lane of each row has its row's sum
-  ADD_DPP(0x142, 0xa);  // rows 1 and 3 add the row before theirs
-  ADD_DPP(0x143, 0xc);  // rows 2 and 3 add the first two
-#undef ADD_DPP
-  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
-}
-
 // Sum over the WAVES waves of a row; `part` is one LDS array per sum.
 template <int WAVES>
 __device__ __forceinline__ float row_sum(float v, float* part) {
