@@ -4,6 +4,8 @@
 
 #include <stdint.h>
 
+#include <initializer_list>
+
 namespace acid {
 
 enum class Fp8Tile { kRows, k256, k128, k64 };

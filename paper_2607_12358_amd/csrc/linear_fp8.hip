@@ -35,6 +35,7 @@ struct Fp8Args {
   float* partial;  // sums of parts of K, for fp8_reduce_kernel
   int32_t M, N, K, groups, split;
   bool whole;  // whole blocks of inputs, 16 bytes of outputs (and residual) at once
+  bool wide;   // four outputs at once
 };
 
 // Sixteen e4m3 values as bf16.
@@ -67,6 +68,16 @@ __device__ __forceinline__ void dma16_from(const void* p, uint32_t lds_byte) {
       "s_mov_b32 m0, %1\n\t"
       "s_nop 0\n\t"
       "global_load_lds_dwordx4 %0, off"
+      :
+      : "v"(p), "s"(lds_byte)
+      : "memory");
+}
+// The same with four bytes a lane.
+__device__ __forceinline__ void dma4_from(const void* p, uint32_t lds_byte) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %0, off"
       :
       : "v"(p), "s"(lds_byte)
       : "memory");
@@ -120,18 +131,7 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
   asm volatile("" : "+v"(lane));  // nothing of this is kept in registers through the stages
   const int lr = lane & 15, lg = lane >> 4;
   auto column = [&](int which, int f) {  // bias (0) or gate (1) of this lane's four outputs
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if constexpr (GENERAL) {
-      const float* v = which ? a.gate : a.bias;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int n = n0 + f * 16 + 4 * lg + r;
-        if (v) x[r] = v[n < a.N ? n : a.N - 1];
-      }
-    } else {  // laid out in LDS when the tile began
-      x = __builtin_bit_cast(f32x4, lds16(columns + (which * FF + f) * 64 + lg * 16));
-    }
-    return x;
+    return __builtin_bit_cast(f32x4, lds16(columns + (which * FF + f) * 64 + lg * 16));
   };
   auto finish = [&](f32x4 y, const f32x4& bias, const f32x4& gate, const f32x4& old) {
     y += bias;
@@ -158,10 +158,18 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
           for (int r = 0; r < 4; ++r) old[r] = at[n + r < a.N ? n + r : a.N - 1];
         }
         const f32x4 y = finish(acc[f][t], bias, gate, old);
-        if (m < a.M) {
+        Out* out = (Out*)a.out + m * a.out_ld + n;
+        if (a.wide) {
+          if (m < a.M && n < a.N) {
+            if constexpr (std::is_same_v<Out, bf16>)
+              *reinterpret_cast<bf16x4*>(out) = bf16x4{(bf16)y[0], (bf16)y[1], (bf16)y[2], (bf16)y[3]};
+            else
+              *reinterpret_cast<f32x4*>(out) = y;
+          }
+        } else if (m < a.M) {
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (n + r < a.N) ((Out*)a.out)[m * a.out_ld + n + r] = (Out)y[r];
+            if (n + r < a.N) out[r] = (Out)y[r];
         }
       }
     }
@@ -397,12 +405,19 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
       for (int f = 0; f < FF; ++f) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
       part[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    if constexpr (!GENERAL && KIND != PARTIAL) {
-      const int n = min(nw + 4 * lane, a.N - 4);
-      if (lane < FF * 4) {
-        dma16_from(a.bias ? (const void*)(a.bias + n) : &kZeros, columns);
-        if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) dma16_from(a.gate + n, columns + FF * 64);
-      }
+    // bias and gate of the wave's outputs, for when the stages are done
+    if constexpr (KIND != PARTIAL) {
+      auto lay = [&](const float* v, uint32_t at) {
+        if constexpr (GENERAL) {
+#pragma unroll
+          for (int j = 0; j < FF * 16; j += 64)
+            dma4_from(v ? v + min(nw + j + lane, a.N - 1) : reinterpret_cast<const float*>(&kZeros), at + j * 4);
+        } else if (lane < FF * 4) {
+          dma16_from(v ? (const void*)(v + min(nw + 4 * lane, a.N - 4)) : &kZeros, at);
+        }
+      };
+      lay(a.bias, columns);
+      if constexpr (KIND == ACID_EPI_GATE_RESIDUAL) lay(a.gate, columns + FF * 64);
     }
     for (int st = it.first; st < it.end; ++st) {
       const uint32_t nxt = buf ^ 1, cur_off = buf * T::STAGE, nxt_off = nxt * T::STAGE;
@@ -478,10 +493,8 @@ __global__ __launch_bounds__(64 * T::WAVES, T::OCC * T::WAVES / 4) void fp8_tile
 #pragma unroll
         for (int t = 0; t < TT; ++t) to[(f * TT + t) * (64 * T::WAVES)] = acc[f][t];
     } else {
-      if constexpr (!GENERAL) {
-        WAIT_DMA(T::LOADS0);  // bias and gate: this many loads were issued after them
-        asm volatile("" ::: "memory");
-      }
+      WAIT_DMA(T::LOADS0);  // bias and gate: this many loads were issued after them
+      asm volatile("" ::: "memory");
       put_tile<Out, KIND, GENERAL, TT, FF>(a, acc, mw, nw, columns, lane);
       WAIT_LDS();  // bias and gate have been read
       asm volatile("" ::: "memory");
@@ -735,9 +748,10 @@ acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t
   const bool whole = K % kFp8Group == 0 && N * os % 16 == 0 && p.out_ld * os % 16 == 0 && (uintptr_t)p.out % 16 == 0 &&
                      (uintptr_t)p.bias % 16 == 0 &&
                      (!update || (p.residual_ld % 4 == 0 && ((uintptr_t)p.residual | (uintptr_t)p.gate) % 16 == 0));
+  const bool wide = N % 4 == 0 && p.out_ld % 4 == 0 && (uintptr_t)p.out % (4 * os) == 0;
   const Fp8Args a = {(const uint8_t*)p.a, (const uint8_t*)p.w, p.a_scales, p.w_scales, p.bias, p.gate,
                      p.residual, p.out, p.a_ld, p.a_scales_ld, p.residual_ld, p.out_ld, (float*)p.workspace, (int32_t)M, N,
-                     K, (int32_t)groups, 1, whole};
+                     K, (int32_t)groups, 1, whole, wide};
   hipError_t e;
   if (p.out_dtype == ACID_BF16)
     e = p.kind == ACID_EPI_BIAS ? launch<bf16, ACID_EPI_BIAS, false>(a, stream)
