@@ -21,14 +21,16 @@ constexpr int kFp8FewRows = 16;
 // round that is not full counts in part; a split adds a second launch and its bytes.  The
 // constants are those that lose least against the best form of each of 185 measured shapes,
 // 17 to 16000 rows, N 64 to 9600, K 128 to 8960: 0.7% on average (exact products 1.7%), 11% at most
-// (28%).  256 x 256 tiles alone would take twice the time.  Microseconds, 256 / 128 / 64, and
+// (28%); 256 x 256 tiles alone lose a factor of two.  Microseconds, 256 / 128 / 64, and
 // 64 in parts:
-//     64 x 1536 x 8960:  89.0 /  42.1 / 27.3, 12 parts  9.5
-//    600 x 4608 x 1536:  22.9 /  11.3 / 11.9
-//   1560 x 1536 x 8960:  92.6 /  43.4 / 37.5, 128 in 4 parts 30.6
-//   4096 x 4608 x 1536:  46.8 /  35.4 / 54.4
-//   8192 x 1536 x 8960: 101.8 / 110.5 / 178.5
-// (64 x 128 tiles too would gain 0.8% on average.)  Up to 16 rows have a kernel of their own.
+//     64 x 1536 x 8960:  88.5 /  40.8 / 27.5, 64 in 8 parts 11.9
+//    300 x 1536 x 8960:  91.6 /  42.0 / 27.9, 64 in 4 parts 18.3
+//    600 x 4608 x 1536:  22.9 /  11.6 / 11.2, 64 in 2 parts 25.2
+//   2500 x 4608 x 8960: 104.4 / 108.5 / 173.0
+//   4096 x 4608 x 1536:  47.5 /  35.9 / 52.3
+//   8200 x 1536 x 8960: 110.2 / 128.8 / 190.3
+// (64 x 128 tiles too would gain 0.8% on average; exact products, whose operands take twice the
+// registers, in 256 x 128 tiles nothing.)  Up to 16 rows have a kernel of their own.
 inline Fp8Form fp8_form(int64_t M, int64_t N, int64_t K, bool exact, int64_t cus) {
   if (M <= kFp8FewRows) return {Fp8Tile::kRows, 1, 0};
   struct Times {
@@ -36,17 +38,16 @@ inline Fp8Form fp8_form(int64_t M, int64_t N, int64_t K, bool exact, int64_t cus
     int tm, tn, occ;
     double base, once, least, each, part;
   };
-  static constexpr Times kTimes[2][3] = {
-      {{Fp8Tile::k256, 256, 256, 1, 0, 10.0, 1.39, 1.39, 0.10},
-       {Fp8Tile::k128, 128, 128, 2, 1.1, 2.4, 0.66, 0.50, 0.74},
-       {Fp8Tile::k64, 64, 64, 4, 2.5, 0.70, 0.361, 0.193, 0.78}},
-      {{Fp8Tile::k256, 256, 128, 1, 0, 10.0, 1.87, 1.87, 0.11},
-       {Fp8Tile::k128, 128, 128, 2, 0, 4.2, 1.23, 0.63, 0.91},
-       {Fp8Tile::k64, 64, 64, 4, 2.9, 1.05, 0.66, 0.36, 0.93}}};
+  static constexpr Times kTimes[] = {{Fp8Tile::k256, 256, 256, 1, 0, 10.0, 1.39, 1.39, 0.10},
+                                     {Fp8Tile::k128, 128, 128, 2, 1.1, 2.4, 0.66, 0.50, 0.74},
+                                     {Fp8Tile::k64, 64, 64, 4, 2.5, 0.70, 0.361, 0.193, 0.78}};
+  static constexpr Times kExact[] = {{Fp8Tile::k128, 128, 128, 2, 0, 4.2, 1.23, 0.63, 0.91},
+                                     {Fp8Tile::k64, 64, 64, 4, 2.9, 1.05, 0.66, 0.36, 0.93}};
   const int64_t blocks = (K + 127) / 128;
-  Fp8Form f = {Fp8Tile::k256, 1, 0};
+  Fp8Form f = {Fp8Tile::k128, 1, 0};
   double best = 1e300;
-  for (const Times& t : kTimes[exact]) {
+  for (int i = 0; i < (exact ? 2 : 3); ++i) {
+    const Times& t = exact ? kExact[i] : kTimes[i];
     const int64_t tiles = (M + t.tm - 1) / t.tm * ((N + t.tn - 1) / t.tn), slots = cus * t.occ;
     for (int split : {1, 2, 3, 4, 6, 8, 12}) {
       const int64_t items = tiles * split;

@@ -671,8 +671,8 @@ hipError_t launch(const Fp8Args& a, hipStream_t s) {
     case Fp8Tile::k128: return launch_tile<Out, KIND, EXACT, Tile<2, 2, 4, 4, 2>>(a, f.split, s);
     case Fp8Tile::k256: break;
   }
-  // (exact products hold their tokens' operands twice: 256 x 128)
-  return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, EXACT ? 4 : 8, 1>>(a, 1, s);
+  if constexpr (EXACT) return hipErrorInvalidValue;  // (not one of its forms)
+  else return launch_tile<Out, KIND, EXACT, Tile<4, 2, 4, 8, 1>>(a, 1, s);
 }
 
 }  // namespace
