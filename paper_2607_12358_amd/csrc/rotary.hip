@@ -111,7 +111,7 @@ constexpr int kWaves = 8, HELD = 4;
 template <typename In, typename Out, int D>
 __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, float* lds) {
   constexpr int LANES = D / 16, TOKENS = 64 / LANES;
-  float2* turns = reinterpret_cast<float2*>(lds);  // [TOKENS][D / 2]
+  float2* turns = reinterpret_cast<float2*>(lds);  // [8][64]: pair i of each lane's eight
   float* part = lds + TOKENS * D;                  // [2][kWaves][TOKENS]
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -119,11 +119,14 @@ __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, f
   const int o = lane % LANES, tt = lane / LANES;
   const int64_t t = t0 + tt < a.tokens ? t0 + tt : a.tokens - 1, row = seq * a.tokens + t;
   const bool live = t0 + tt < a.tokens;
-  // the dims of this lane's two runs of eight
-  int d0 = 16 * o, d1 = d0 + 8;
-  if (a.halves && 8 * o < a.pairs) {
-    d0 = 8 * o;
-    d1 = a.pairs + d0;
+  // this lane's two runs of eight dims, and its pairs, in two runs of four: neighbouring lanes
+  // have neighbouring runs (of whole lines), but in halves past the pairs
+  int d0 = 8 * o, d1 = D / 2 + d0, p0 = 4 * o, p1 = D / 4 + p0;
+  if (a.halves) {
+    p0 = 8 * o;
+    p1 = p0 + 4;
+    d0 = 8 * o < a.pairs ? 8 * o : 16 * o;  // 2 pairs + 16 (o - pairs / 8)
+    d1 = d0 + (8 * o < a.pairs ? a.pairs : 8);
   }
   const int nq = a.q ? a.heads : 0, nk = a.k ? a.kv_heads : 0, n = nq + nk;
   auto source = [&](int u) {
@@ -147,7 +150,8 @@ __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, f
       turn -= rint(turn);
       sincospif(2.0f * (float)turn, &cs.y, &cs.x);
     }
-    turns[i] = cs;
+    const int run = p / 4, lane_of = a.halves ? run / 2 : run % LANES, second = a.halves ? run % 2 : run / LANES;
+    turns[(4 * second + p % 4) * 64 + i / (D / 2) * LANES + lane_of] = cs;
   }
   if (a.norm == ACID_HEAD_NORM_RMS_ROW) {
     float sums[2] = {0.f, 0.f};
@@ -186,7 +190,7 @@ __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, f
   }
   float2 cs[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) cs[i] = turns[tt * (D / 2) + 8 * o + i];
+  for (int i = 0; i < 8; ++i) cs[i] = turns[i * 64 + lane];
 
   auto finish = [&](const Held<In>& h, int u) {
     const bool is_q = u < nq;
@@ -228,7 +232,7 @@ __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, f
     }
     const float scale = is_q ? a.q_scale : 1.f;
     auto turn = [&](float& x, float& y, int i) {
-      const bool turned = 8 * o + i < a.pairs;
+      const bool turned = (i < 4 ? p0 + i : p1 + i - 4) < a.pairs;
       const float nx = x * cs[i].x - y * cs[i].y, ny = x * cs[i].y + y * cs[i].x;
       x = scale * (turned ? nx : x);
       y = scale * (turned ? ny : y);
@@ -258,10 +262,10 @@ __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, f
 }
 
 // V^T of 64 tokens and 64 dims of a head, by way of LDS: eight dims of a token a thread
-// in, eight tokens of a dim out.
+// in, eight tokens of a dim out.  The eight tokens j of dim d lie at place j ^ (d / 8) % 8 of
+// the dim's row, so that a wave's writes of one token's dims meet different banks.
 template <typename In, typename Out, int D>
 __device__ __forceinline__ void transpose_v(const HeadArgs& a, int64_t group, float* lds) {
-  constexpr int PITCH = 64 + 16 / sizeof(Out);  // of a dim's tokens
   Out* tile = reinterpret_cast<Out*>(lds);
   const int tid = threadIdx.x, units = a.kv_heads * (D / 64);
   const int64_t per_seq = a.v_tiles * units, seq = group / per_seq, rest = group - seq * per_seq;
@@ -270,15 +274,15 @@ __device__ __forceinline__ void transpose_v(const HeadArgs& a, int64_t group, fl
   const int head = part / (D / 64), dim0 = part % (D / 64) * 64;
   const int left = (int)(a.tokens - t0 < 64 ? a.tokens - t0 : 64);
   {
-    const int r = tid / 8, c = tid % 8 * 8;
+    const int r = tid / 8, c = tid % 8;
     float v[8];
-    load8((const In*)a.v + (seq * a.tokens + t0 + (r < left ? r : left - 1)) * a.v_ld + head * D + dim0 + c, v);
+    load8((const In*)a.v + (seq * a.tokens + t0 + (r < left ? r : left - 1)) * a.v_ld + head * D + dim0 + c * 8, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) tile[(c + e) * PITCH + r] = (Out)v[e];
+    for (int e = 0; e < 8; ++e) tile[(c * 8 + e) * 64 + (r / 8 ^ c) * 8 + r % 8] = (Out)v[e];
   }
   __syncthreads();
   const int dim = tid / 8, c = tid % 8 * 8;
-  const Out* from = tile + dim * PITCH + c;
+  const Out* from = tile + dim * 64 + (tid % 8 ^ dim / 8) * 8;
   Out* to = (Out*)a.vt + seq * a.vt_seq + head * a.vt_head + (dim0 + dim) * a.vt_row + t0 + c;
   if (a.vt_wide && c + 8 <= left) {
 #pragma unroll
@@ -291,7 +295,7 @@ __device__ __forceinline__ void transpose_v(const HeadArgs& a, int64_t group, fl
 
 template <typename In, typename Out, int D>
 __global__ __launch_bounds__(64 * kWaves) void rotary_qkv_kernel(HeadArgs a) {
-  constexpr int TURNS = 1024 / D * D + 2 * kWaves * (1024 / D), TILE = 64 * (64 + 16 / sizeof(Out)) * sizeof(Out) / 4;
+  constexpr int TURNS = 1024 / D * D + 2 * kWaves * (1024 / D), TILE = 64 * 64 * sizeof(Out) / 4;
   __shared__ __attribute__((aligned(16))) float lds[TURNS > TILE ? TURNS : TILE];
   if ((int64_t)blockIdx.x < a.qk_groups)
     rotate_heads<In, Out, D>(a, blockIdx.x, lds);
