@@ -45,15 +45,17 @@ __device__ __forceinline__ void load8(const float* p, float* v) {
     v[4 + i] = b[i];
   }
 }
+// Streaming stores: Q and K are not read again before they have left L2 (131 -> 127 us; V^T's, of
+// 128 bytes a row, take 16 us more so).
 __device__ __forceinline__ void store8(bf16* p, const float* v) {
   bf16x8 w;
 #pragma unroll
   for (int i = 0; i < 8; ++i) w[i] = (bf16)v[i];
-  *reinterpret_cast<bf16x8*>(p) = w;
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), reinterpret_cast<u32x4*>(p));
 }
 __device__ __forceinline__ void store8(float* p, const float* v) {
-  *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-  *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4*>(p));
+  __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4*>(p + 4));
 }
 
 // Sixteen values of a head as they were loaded: two runs of eight.
