@@ -581,7 +581,7 @@ acid_status acid_linear_w4(int32_t x_dtype, int64_t M, int32_t N, int32_t K, int
  * and a multiple of 4 (entries past `rows` are neither written nor used).
  *   scale = max(max |x| / 448, 2^-126), code = x (1 / scale) to nearest, ties to even
  * A group with an infinity or a NaN gets scale NaN and codes that mean nothing.  K is a
- * multiple of 16, <= 2^22, ceil(rows / 32) ceil(K / 128) <= 2^26; matrices' rows lie
+ * multiple of 16, <= 2^22, ceil(rows / 32) ceil(K / 128) < 2^26; matrices' rows lie
  * whole 16 bytes apart, buffers are 16-byte aligned and apart from one another.
  *
  * acid_quantize_fp8: rows x [rows][x_ld] in x_dtype. */
@@ -625,8 +625,10 @@ typedef struct {
 /* y = a w^T + bias with the rows' and the weights' scales, accumulated in fp32;
  * out = y (BIAS), GELU_tanh(y) (BIAS_GELU), residual + gate (.) y (GATE_RESIDUAL).  Any M
  * from a single row on (<= 2^24) and any N; K a multiple of 16, K and N <= 2^22, ceil(M /
- * 64) ceil(N / 64) < 2^23; a_ld < 2^24.  Plain and GELU outputs in fp32 come from exact products and fp32 sums; bf16 ones
- * and the gated y from the 8-bit matrix units, whose sums are about 1.4e-5 off.  out
+ * 64) ceil(N / 64) < 2^23; a_ld < 2^24.  Plain and GELU outputs in fp32 come from exact
+ * products and fp32 sums; bf16 ones and the gated y from the 8-bit matrix units, whose
+ * sums are about 1.4e-5 off.  w_scales, bias, gate, residual and out are aligned to an
+ * element (16 bytes, rows included, are faster), a, a_scales and w to 16 bytes.  out
  * lies apart from everything but the residual.  Workspace:
  * acid_linear_fp8_workspace_needed(...) bytes (0: may be NULL), ACID_ERR_SHAPE if
  * it is smaller.  A NaN code or scale makes NaN the outputs it belongs to, no others. */
@@ -671,7 +673,7 @@ typedef struct {
  * rest in fp32, rounded once.  Position 0 on every axis turns by nothing (text).
  * head_dim 64 or 128; pairs <= head_dim / 2 in all, in pairing 1 a multiple of 8.
  * Contiguous q_out [n_seq][heads][tokens][d] is attention's; other strides write
- * into a cache's rows or keep tokens outermost.  q, k, v, q_out, k_out, weights and
+ * into a cache's rows or keep tokens outermost, sequences beyond both.  q, k, v, q_out, k_out, weights and
  * biases 16-byte aligned, rows and strides of the first five whole 16 bytes; vt as its
  * elements.  Outputs apart from all else, but q_out may be q's own rows (of its type,
  * tokens outermost), k_out k's. */

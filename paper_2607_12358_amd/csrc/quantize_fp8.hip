@@ -240,10 +240,10 @@ __global__ __launch_bounds__(256) void quantize_fp8_weight_kernel(const float* _
 acid_status check_rows(int64_t rows, int64_t K, int64_t x_ld, int64_t x_size, int64_t codes_ld,
                        int64_t scales_ld) {
   if (rows < 0 || K < 1) return set_error(ACID_ERR_INVALID_ARG, "fp8: rows < 0 or K < 1");
-  if (K % 16 || K > (1 << 22) || (rows + 31) / 32 * fp8_groups(K) > (1 << 26))
+  if (K % 16 || K > (1 << 22) || (rows + 31) / 32 * fp8_groups(K) >= (1 << 26))
     return set_error(ACID_ERR_SHAPE,
                      "fp8: K %lld must be a multiple of 16, <= 2^22, and ceil(rows / 32) "
-                     "ceil(K / 128) <= 2^26", (long long)K);
+                     "ceil(K / 128) < 2^26", (long long)K);
   constexpr int64_t most = (int64_t)1 << 32;
   if (x_ld < K || x_ld * x_size % 16 || x_ld > most || codes_ld < K || codes_ld % 16 ||
       codes_ld > most)

@@ -5,7 +5,8 @@
 // Pair i of a head belongs to one axis; its angle is positions[axis][token]
 // freqs[i], taken in 64 bits and in turns, so that far positions keep their
 // fraction; sine and cosine of that are taken in 32 bits.  Bound by HBM: each row is
-// read and written once.
+// read and written once.  32760 tokens of 12 + 12 + 12 heads of 128, bf16, norm over the row, 604
+// MB: 127 us, 4.75 TB/s, where a copy makes 5.2; one token of 16 + 4 + 4 heads of 64: 4.3 us.
 #include <cmath>
 #include <type_traits>
 
@@ -106,9 +107,11 @@ __device__ __forceinline__ float head_sum(float v) {
 
 // Q and K of 64 / (D / 16) tokens: a lane holds sixteen values of a head, eight pairs, and
 // the eight waves take the heads in turn.  Up to HELD heads a wave are loaded at once and
-// stay in registers between their norm's sum and their rotation (more of them are read
-// again: 32 heads of Q and K together are 8 x HELD).  The angles' sines and cosines are made once a
-// token and shared by way of LDS, while the heads are on their way.
+// stay in registers between their norm's sum and their rotation; past 32 heads of Q and K
+// together the rest is read again.  The angles' sines and cosines are made once a token and
+// shared by way of LDS, while the heads are on their way.  (At the size above: heads held, loads
+// before the angles and 16-byte stores of V^T 140 us of 212, the lanes' order in a head and
+// the layout in LDS 131, streaming stores 127.)
 constexpr int kWaves = 8, HELD = 4;
 template <typename In, typename Out, int D>
 __device__ __forceinline__ void rotate_heads(const HeadArgs& a, int64_t group, float* lds) {
@@ -314,8 +317,7 @@ hipError_t launch(int d, const HeadArgs& a, unsigned grid, hipStream_t s) {
   return hipGetLastError();
 }
 
-// An output as rows of bytes: blocks of heads side by side, or whole heads one after
-// another; as one run of bytes where it is neither.
+// An output as rows of bytes, one for each token, head or sequence.
 struct Rows {
   const void* p;
   int64_t rows, width, ld;
@@ -326,12 +328,10 @@ Rows input_rows(const void* p, int64_t rows, int64_t width, int64_t ld, int64_t 
 }
 Rows output_rows(const void* p, int64_t n_seq, int64_t heads, int64_t rows, int64_t width, int64_t head,
                  int64_t row, int64_t seq, int64_t size) {
-  if (head == width && (n_seq == 1 || seq == rows * row))  // token-major
-    return {p, n_seq * rows, heads * width * size, row * size};
-  if (row == width && (n_seq == 1 || seq == heads * head))  // head-major
-    return {p, n_seq * heads, rows * width * size, head * size};
-  const int64_t all = ((n_seq - 1) * seq + (heads - 1) * head + (rows - 1) * row + width) * size;
-  return {p, 1, all, all};
+  const int64_t token = (heads - 1) * head + width, whole = (rows - 1) * row + width;
+  if (row >= token && (n_seq == 1 || seq == rows * row)) return {p, n_seq * rows, token * size, row * size};
+  if (head >= whole && (n_seq == 1 || seq == heads * head)) return {p, n_seq * heads, whole * size, head * size};
+  return {p, n_seq, ((heads - 1) * head + whole) * size, seq * size};
 }
 // Whether no two values of an output share an address: one axis within the
 // other, and a sequence beyond both.

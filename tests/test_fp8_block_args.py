@@ -25,7 +25,7 @@ def _rows(lib, **kw):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(dtype=2), BAD), (dict(rows=-1), BAD), (dict(K=0), BAD), (dict(K=250), SHAPE), (dict(K=1 << 23, xld=1 << 23, cld=1 << 23), SHAPE),
-    (dict(rows=1 << 31, sld=1 << 31), SHAPE), (dict(xld=255), SHAPE), (dict(xld=260), SHAPE), (dict(xld=1 << 33), SHAPE),
+    (dict(rows=1 << 31, sld=1 << 31), SHAPE), (dict(rows=1 << 31, K=16, sld=1 << 31), SHAPE), (dict(xld=255), SHAPE), (dict(xld=260), SHAPE), (dict(xld=1 << 33), SHAPE),
     (dict(dtype=L.ACID_F32, xld=258), SHAPE), (dict(cld=240), SHAPE), (dict(cld=264), SHAPE), (dict(sld=8), SHAPE), (dict(sld=13), SHAPE),
     (dict(x=None), BAD), (dict(codes=None), BAD), (dict(scales=None), BAD), (dict(x=G + 8), BAD), (dict(codes=2 * G + 8), BAD),
     (dict(scales=3 * G + 4), BAD), (dict(codes=G), BAD), (dict(scales=G + 512), BAD), (dict(scales=2 * G + 256), BAD)])

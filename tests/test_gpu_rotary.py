@@ -132,6 +132,32 @@ def test_layouts_give_the_same_values(pairs):
     assert torch.equal(qkv[:, 512:].reshape(37, 2, 64).permute(1, 2, 0), vt)
 
 
+def test_one_buffer_for_both_caches():
+    """K and V^T side by side for each head, or for each sequence: apart, though their reaches cross."""
+    P = need_gpu()
+    _, (q, k, v), (_, ko, vt), pos, freqs, sections = _some(P, tokens=37)
+    P.rotary_qkv(None, k, v, pos, freqs, sections, None, ko, vt)
+    cap, d = 48, 64
+    for n_seq in (1, 2):
+        rows = [torch.cat([t] * n_seq) for t in (k, v)]
+        p = torch.cat([pos] * n_seq, 1).contiguous()
+        for by_head in (True, False):
+            head = (2 if by_head else 1) * cap * d
+            seq = 4 * cap * d
+            buf = torch.full((n_seq * seq,), 7.0, device="cuda").bfloat16()
+            kc = buf.as_strided((n_seq, 2, 37, d), (seq, head, d, 1), 0)
+            vc = buf.as_strided((n_seq, 2, d, 37), (seq, head, cap, 1), (1 if by_head else 2) * cap * d)
+            P.rotary_qkv(None, *rows, p, freqs, sections, None, kc, vc)
+            for s in range(n_seq):
+                assert torch.equal(kc[s], ko) and torch.equal(vc[s], vt)
+            left = buf.clone()
+            left.as_strided(kc.shape, kc.stride(), kc.storage_offset()).fill_(7.0)
+            left.as_strided(vc.shape, vc.stride(), vc.storage_offset()).fill_(7.0)
+            assert (left == 7.0).all()
+            with pytest.raises(P.AcidError, match="outputs overlap"):
+                P.rotary_qkv(None, *rows, p, freqs, sections, None, kc, buf.as_strided(vc.shape, vc.stride(), 36 * d))
+
+
 @pytest.mark.parametrize("norm", ["none", "rms_row"])
 def test_in_place_rows_norm(norm):
     P = need_gpu()
