@@ -14,7 +14,20 @@
 // that are 1.4e-5 off, against 2^-9 for the rounding to bf16 that follows and some 2^-5
 // for the operands' own.  Outputs in bf16, and updates of a residual, take them.
 // Plain fp32 outputs take the bf16 instruction on operands converted on the way, which
-// is exact: products and sums in fp32.
+// is exact: products and sums in fp32, in about twice the time.
+//
+// Microseconds on one MI355X, 8-bit products to bf16 (a register-only stream of the
+// instruction makes 3.8 PFLOP/s, the library's product without block scales 2.4 to 3.3):
+//   32760 x 4608 x 1536   227 (2.04 PFLOP/s)     8192 x 8192 x 8192  434 (2.53)
+//   32760 x 1536 x 8960   370 (2.44); onto a residual in fp32 442
+//   64 x 1536 x 8960  9.5    1 x 8960 x 1536  4.7    1 x 28672 x 8192  38.8 (6.1 TB/s)
+// The large ones run at 1.8 GHz with the matrix units 60% busy (the library's: 1.7 and
+// 82%).  At 32760 x 1536 x 8960 every part that was left out for a timing took its time with it,
+// whatever else was left out: loads of operands 15%, reads of LDS 20%, the scales'
+// multiply-adds 8%, barriers 3%, the outputs 6%.  Leaving out the waits, wave priorities
+// and other orders of the loads change nothing.  So the bound is what all of them share,
+// most likely the power of the card, and not a latency.
+
 #include <algorithm>
 #include <type_traits>
 
@@ -125,6 +138,8 @@ struct Tile {
 // outputs 4 (l / 16) .. + 3 of token l % 16.
 // Whole 16 bytes: fp32 as they are; two bf16 blocks side by side exchange halves between
 // neighbouring rows of 16 lanes, so that each lane has eight outputs of one of them.
+// Streaming stores: ordinary ones push the operands out of L2 (with groups of four token
+// tiles for two, 32760 x 4608 x 1536 256 -> 232 us).
 template <typename Out, int KIND, bool GENERAL, int TT, int FF>
 __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT], int64_t m0, int n0,
                                          uint32_t columns, int lane) {
@@ -236,8 +251,9 @@ __device__ __forceinline__ void put_tile(const Fp8Args& a, f32x4 (&acc)[FF][TT],
 // scales, loaded straight into one of two buffers in LDS.  Two barriers a stage: each frees
 // what all waves have read, a half of its buffer (part 0, then part 1), which is then
 // filled for the stage after the next, one load at a time between the products; so
-// loads run one and a half stages ahead, into the next tile.  (All at once behind
-// the barrier, they hold back the waves that issue them: see below.)
+// loads run one and a half stages ahead, into the next tile.  (32760 x 1536 x 8960, by one
+// wave of each SIMD: one barrier a stage and loads at once behind it 451 us, two barriers 397,
+// spread 391; by all waves, spread, from tile to tile 380.)
 // Row r's 16-byte chunk c lies at slot c ^ (r / 2 % 8), so that sixteen rows of one
 // chunk cover all 64 banks.  Rows past M and N are copies of the last.  A lane's operand of
 // a 16 x 16 x 128 product is chunks g and g + 4 (g its row of 16 lanes) of both tiles'
@@ -518,7 +534,11 @@ __device__ __forceinline__ void put_one(const Fp8Args& a, float y, int64_t m, in
 // Up to 16 rows, bound by reading the weights once.  A workgroup has 16 outputs; its WAVES
 // waves take the blocks of inputs in turn, and their sums are added in wave order.  A wave's
 // operands go by way of a part of LDS that is its own: whole lines, DEEP blocks ahead,
-// laid out as the tiles' above.  X: eights of rows.
+// laid out as the tiles' above (each lane's own 16 bytes straight into registers: 1 x 8960 x
+// 1536 7.2 us for 4.7, 1 x 28672 x 8192 53 for 39, 16 rows of it 71 for 46).  Eight waves and
+// two blocks ahead are best or within 11% from 4608 x 1536 to 28672 x 8192; four waves lose 25%
+// where the inputs are long (1536 x 8960 6.2 us for 5.0), sixteen where they are short (5.1
+// for 3.9).  X: eights of rows.
 template <typename Out, int KIND, bool EXACT, int WAVES, int DEEP, int X>
 __global__ __launch_bounds__(64 * WAVES) void fp8_rows_kernel(Fp8Args a) {
   constexpr int BLOCK = 2048 + X * 1024 + 128, LOADS = 2 + X + 1;
@@ -607,7 +627,9 @@ hipError_t launch_rows(const Fp8Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The parts' sums of a split tile, added in order, then its outputs: four a thread.
+// The parts' sums of a split tile, added in order, then its outputs: four a thread.  Costs
+// some 3.3 us, its launch for the most part, where the split saves more (64 x 1536 x 8960 in
+// 64 x 64 tiles 27 -> 9.5 us).
 template <typename Out, int KIND, typename T>
 __global__ __launch_bounds__(256) void fp8_reduce_kernel(Fp8Args a) {
   constexpr int EACH = T::TM * T::TN / 4, THREADS = 64 * T::WAVES;
