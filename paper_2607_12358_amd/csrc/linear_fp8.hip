@@ -14,13 +14,14 @@
 // that are 1.4e-5 off, against 2^-9 for the rounding to bf16 that follows and some 2^-5
 // for the operands' own.  Outputs in bf16, and updates of a residual, take them.
 // Plain fp32 outputs take the bf16 instruction on operands converted on the way, which
-// is exact: products and sums in fp32, in about twice the time.
+// is exact: products and sums in fp32, in about twice the time (32760 x 1536 x 8960 773 us
+// for 367).
 //
 // Microseconds on one MI355X, 8-bit products to bf16 (a register-only stream of the
 // instruction makes 3.8 PFLOP/s, the library's product without block scales 2.4 to 3.3):
-//   32760 x 4608 x 1536   227 (2.04 PFLOP/s)     8192 x 8192 x 8192  434 (2.53)
-//   32760 x 1536 x 8960   370 (2.44); onto a residual in fp32 442
-//   64 x 1536 x 8960  9.5    1 x 8960 x 1536  4.7    1 x 28672 x 8192  38.8 (6.1 TB/s)
+//   32760 x 4608 x 1536   227 (2.04 PFLOP/s)     8192 x 8192 x 8192  426 (2.58)
+//   32760 x 1536 x 8960   367 (2.46); onto a residual in fp32 445
+//   64 x 1536 x 8960  12.5   1 x 8960 x 1536  4.7    1 x 28672 x 8192  38.8 (6.1 TB/s)
 // The large ones run at 1.8 GHz with the matrix units 60% busy (the library's: 1.7 and
 // 82%).  At 32760 x 1536 x 8960 every part that was left out for a timing took its time with it,
 // whatever else was left out: loads of operands 15%, reads of LDS 20%, the scales'
@@ -629,7 +630,7 @@ hipError_t launch_rows(const Fp8Args& a, hipStream_t s) {
 
 // The parts' sums of a split tile, added in order, then its outputs: four a thread.  Costs
 // some 3.3 us, its launch for the most part, where the split saves more (64 x 1536 x 8960 in
-// 64 x 64 tiles 27 -> 9.5 us).
+// 64 x 64 tiles 27.5 -> 11.9 us).
 template <typename Out, int KIND, typename T>
 __global__ __launch_bounds__(256) void fp8_reduce_kernel(Fp8Args a) {
   constexpr int EACH = T::TM * T::TN / 4, THREADS = 64 * T::WAVES;
