@@ -50,7 +50,8 @@ def _weights(norm, heads, kv, d):
 @pytest.mark.parametrize("tokens,heads,kv,d,sections", [
     (1, 1, 1, 64, (32,)), (1, 16, 4, 64, (32,)), (1, 12, 12, 128, (22, 21, 21)), (7, 3, 3, 128, (16, 24, 24)),
     (15, 5, 1, 64, (8, 8)), (17, 2, 2, 64, (16, 8, 8)), (63, 4, 2, 128, (64,)), (64, 1, 1, 128, (0, 32, 32)),
-    (65, 7, 7, 64, (8, 4, 4)), (130, 24, 8, 128, (8, 8, 8, 8)), (257, 40, 40, 128, (22, 21, 21)), (100, 33, 3, 64, (32,))])
+    (65, 7, 7, 64, (8, 4, 4)), (130, 24, 8, 128, (8, 8, 8, 8)), (257, 40, 40, 128, (22, 21, 21)), (100, 33, 3, 64, (32,)),
+    (3, 1024, 1024, 64, (12, 10, 10))])
 @pytest.mark.parametrize("pairs", ["adjacent", "halves"])
 @pytest.mark.parametrize("norm", ["none", "rms", "layer", "rms_row"])
 @pytest.mark.parametrize("din,dout", [(BF16, BF16), (F32, F32), (F32, BF16), (BF16, F32)], ids=["bf16", "f32", "f32-bf16", "bf16-f32"])
@@ -125,8 +126,8 @@ def test_layouts_give_the_same_values(pairs):
         assert torch.equal(x[0], y)
         assert torch.equal(x[1], y.flip(2 if y is vt else 1))
     # in place, tokens outermost
-    P.rotary_qkv(q, k, None, pos, freqs, sections, q.reshape(37, 6, 64).transpose(0, 1) if False else
-                 qkv.as_strided((6, 37, 64), (64, 640, 1)), qkv.as_strided((2, 37, 64), (64, 640, 1), 384), None, **kw)
+    P.rotary_qkv(q, k, None, pos, freqs, sections, qkv.as_strided((6, 37, 64), (64, 640, 1)),
+                 qkv.as_strided((2, 37, 64), (64, 640, 1), 384), None, **kw)
     assert torch.equal(qkv[:, :384].reshape(37, 6, 64).transpose(0, 1), qo)
     assert torch.equal(qkv[:, 384:512].reshape(37, 2, 64).transpose(0, 1), ko)
     assert torch.equal(qkv[:, 512:].reshape(37, 2, 64).permute(1, 2, 0), vt)
@@ -225,7 +226,7 @@ def test_refusals():
     ok = dict(q=q, k=k, v=v, positions=pos, freqs=freqs, sections=sections, q_out=qo, k_out=ko, vt=vt)
     P.rotary_qkv(**ok)
     for kw in (dict(norm="l2"), dict(pairs="other"), dict(sections=()), dict(sections=(8,) * 5), dict(q=None), dict(vt=None),
-               dict(q=q.float()), dict(ko=None) if False else dict(k_out=ko.float()), dict(positions=pos.long()), dict(positions=pos[:2]),
+               dict(q=q.float()), dict(k_out=ko.float()), dict(positions=pos.long()), dict(positions=pos[:2]),
                dict(freqs=freqs.float()), dict(freqs=freqs[:3]), dict(q_out=qo[:, :36]), dict(vt=vt.transpose(1, 2)),
                dict(q_weight=torch.ones(3, device="cuda"), norm="rms"), dict(q_out=qo.transpose(1, 2).contiguous().transpose(1, 2))):
         with pytest.raises(ValueError):
