@@ -30,9 +30,14 @@ constexpr int kFp8FewRows = 16;
 //   4096 x 4608 x 1536:  47.5 /  35.9 / 52.3
 //   8200 x 1536 x 8960: 110.2 / 128.8 / 190.3
 // (64 x 128 tiles too would gain 0.8% on average; exact products, whose operands take twice the
-// registers, in 256 x 128 tiles nothing.)  Up to 16 rows have a kernel of their own.
+// registers, in 256 x 128 tiles nothing.)  Up to 16 rows have a kernel of their own, and up to
+// 32 where its workgroups, of 16 outputs and one a CU, take less than two rounds (its bf16
+// outputs, then exact ones, / 64 x 64 tiles, parts among them):
+//   32 x 1536 x 1536  3.3, 3.6 /  7.4,  8.5       32 x 8960 x 1536   8.3,  8.8 /  7.8, 10.9
+//   32 x 4608 x 1536  6.0, 6.3 /  7.7, 10.8       32 x 8192 x 8192  20.6, 21.4 / 19.6, 22.5
+//   32 x 1536 x 8960  7.5, 8.3 / 11.2, 13.5       32 x 28672 x 8192 64.7, 66.6 / 49.1, 57.8
 inline Fp8Form fp8_form(int64_t M, int64_t N, int64_t K, bool exact, int64_t cus) {
-  if (M <= kFp8FewRows) return {Fp8Tile::kRows, 1, 0};
+  if (M <= kFp8FewRows || (M <= 2 * kFp8FewRows && (N + 15) / 16 < 2 * cus)) return {Fp8Tile::kRows, 1, 0};
   struct Times {
     Fp8Tile tile;
     int tm, tn, occ;

@@ -533,19 +533,19 @@ __device__ __forceinline__ void put_one(const Fp8Args& a, float y, int64_t m, in
   ((Out*)a.out)[m * a.out_ld + n] = (Out)y;
 }
 
-// Up to 16 rows, bound by reading the weights once.  A workgroup has 16 outputs; its WAVES
+// Up to 32 rows, bound by reading the weights once.  A workgroup has 16 outputs; its WAVES
 // waves take the blocks of inputs in turn, and their sums are added in wave order.  A wave's
 // operands go by way of a part of LDS that is its own: whole lines, DEEP blocks ahead,
 // laid out as the tiles' above (each lane's own 16 bytes straight into registers: 1 x 8960 x
 // 1536 7.2 us for 4.7, 1 x 28672 x 8192 53 for 39, 16 rows of it 71 for 46).  Eight waves and
 // two blocks ahead are best or within 11% from 4608 x 1536 to 28672 x 8192; four waves lose 25%
 // where the inputs are long (1536 x 8960 6.2 us for 5.0), sixteen where they are short (5.1
-// for 3.9).  X: eights of rows.
+// for 3.9).  X: eights of rows (LDS for one workgroup a CU with four, two with fewer).
 template <typename Out, int KIND, bool EXACT, int WAVES, int DEEP, int X>
 __global__ __launch_bounds__(64 * WAVES) void fp8_rows_kernel(Fp8Args a) {
-  constexpr int BLOCK = 2048 + X * 1024 + 128, LOADS = 2 + X + 1;
+  constexpr int BLOCK = 2048 + X * 1024 + 128, LOADS = 2 + X + 1, TT = (X + 1) / 2;
   __shared__ __attribute__((aligned(1024))) uint8_t ring[WAVES * DEEP * BLOCK];
-  static_assert(sizeof(ring) >= WAVES * 1024 && sizeof(ring) <= 160 * 1024 && LOADS * (DEEP - 1) <= 63, "ring");
+  static_assert(sizeof(ring) >= WAVES * TT * 1024 && TT * 64 <= 128 && sizeof(ring) <= 160 * 1024 && LOADS * (DEEP - 1) <= 63, "ring");
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lg = lane >> 4;
@@ -558,7 +558,7 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_rows_kernel(Fp8Args a) {
 #pragma unroll
   for (int i = 0; i < X; ++i) from[2 + i] = a.a + (int64_t)std::min(8 * i + row, a.M - 1) * a.a_ld;
   const float* sw = a.w_scales + (int64_t)(n0 / kFp8Group) * a.groups;
-  const float* sx = a.a_scales + std::min(4 * (lane & 3), (a.M - 1) & ~3);
+  const float* sx = a.a_scales + std::min(4 * (lane & (4 * TT - 1)), (a.M - 1) & ~3);
   auto load = [&](int b, uint32_t at) {
 #pragma unroll
     for (int i = 0; i < 2 + X; ++i) {
@@ -566,9 +566,11 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_rows_kernel(Fp8Args a) {
       const bool in = !tail || b + 1 < a.groups || k < tail;
       dma16_from(in ? from[i] + (int64_t)b * kFp8Group + k : reinterpret_cast<const uint8_t*>(&kZeros), at + i * 1024);
     }
-    if (lane < 4) dma16_from(sx + b * a.a_scales_ld, at + (2 + X) * 1024);
+    if (lane < 4 * TT) dma16_from(sx + b * a.a_scales_ld, at + (2 + X) * 1024);
   };
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  f32x4 acc[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   const uint32_t swz = (uint32_t)((lg ^ (lr >> 1)) * 16);
 #pragma unroll
   for (int i = 0; i < DEEP; ++i)
@@ -580,40 +582,51 @@ __global__ __launch_bounds__(64 * WAVES) void fp8_rows_kernel(Fp8Args a) {
     else WAIT_DMA(0);
     asm volatile("" ::: "memory");
     const uint32_t w_at = at + lr * kFp8Group + swz, x_at = at + 2048 + lr % (8 * X) * kFp8Group + swz;
-    const Pair w = {{lds16(w_at), lds16(w_at ^ 64)}}, x = {{lds16(x_at), lds16(x_at ^ 64)}};
-    const float s = lds4(at + (2 + X) * 1024 + lr * 4) * s_out;
+    const Pair w = {{lds16(w_at), lds16(w_at ^ 64)}};
+    Pair x[TT];
+    float scale[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+      x[t] = Pair{{lds16(x_at + t * 2048), lds16((x_at ^ 64) + t * 2048)}};
+      scale[t] = lds4(at + (2 + X) * 1024 + (t * 16 + lr) * 4) * s_out;
+    }
     WAIT_LDS();
     asm volatile("" ::: "memory");
     if (b + DEEP * WAVES < a.groups) load(b + DEEP * WAVES, at);
     at = at + BLOCK == mine + DEEP * BLOCK ? mine : at + BLOCK;
-    f32x4 part = {0.f, 0.f, 0.f, 0.f};
-    if constexpr (EXACT) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        bf16x8 bw[2], bx[2];
-        to_bf16(w.v[j], bw);
-        to_bf16(x.v[j], bx);
+    for (int t = 0; t < TT; ++t) {
+      f32x4 part = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (EXACT) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[h], bx[h], part, 0, 0, 0);
+        for (int j = 0; j < 2; ++j) {
+          bf16x8 bw[2], bx[2];
+          to_bf16(w.v[j], bw);
+          to_bf16(x[t].v[j], bx);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[h], bx[h], part, 0, 0, 0);
+        }
+      } else {
+        part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+            __builtin_bit_cast(i32x8, w), __builtin_bit_cast(i32x8, x[t]), part, 0, 0, 0, 0, 0, 0);
       }
-    } else {
-      part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-          __builtin_bit_cast(i32x8, w), __builtin_bit_cast(i32x8, x), part, 0, 0, 0, 0, 0, 0);
-    }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) acc[r] = fmaf(s, part[r], acc[r]);
+      for (int r = 0; r < 4; ++r) acc[t][r] = fmaf(scale[t], part[r], acc[t][r]);
+    }
   }
   __syncthreads();  // (every load has landed)
   float* sums = reinterpret_cast<float*>(ring);  // [wave][token][output]
-  *reinterpret_cast<f32x4*>(sums + wave * 256 + lr * 16 + 4 * lg) = acc;
+#pragma unroll
+  for (int t = 0; t < TT; ++t)
+    *reinterpret_cast<f32x4*>(sums + (wave * TT + t) * 256 + lr * 16 + 4 * lg) = acc[t];
   __syncthreads();
   for (int i = threadIdx.x; i < a.M * 16; i += 64 * WAVES) {
     const int n = n0 + i % 16;
     if (n >= a.N) continue;
     float y = 0.f;
 #pragma unroll
-    for (int v = 0; v < WAVES; ++v) y += sums[v * 256 + i];
+    for (int v = 0; v < WAVES; ++v) y += sums[v * TT * 256 + i];
     put_one<Out, KIND>(a, y, i / 16, n);
   }
 }
@@ -624,8 +637,10 @@ hipError_t launch_rows(const Fp8Args& a, hipStream_t s) {
   const dim3 grid((a.N + 15) / 16), block(64 * WAVES);
   if (a.M <= 8)
     hipLaunchKernelGGL((fp8_rows_kernel<Out, KIND, EXACT, WAVES, DEEP, 1>), grid, block, 0, s, a);
-  else
+  else if (a.M <= 16)
     hipLaunchKernelGGL((fp8_rows_kernel<Out, KIND, EXACT, WAVES, DEEP, 2>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((fp8_rows_kernel<Out, KIND, EXACT, WAVES, DEEP, 4>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 

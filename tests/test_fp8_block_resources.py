@@ -6,7 +6,7 @@ from test_kernel_resources import kernels  # noqa: F401  (fixture)
 
 # Waves of a workgroup and workgroups per CU that a kernel's split was chosen for.
 RESIDENT = {"4TileILi4ELi2ELi4ELi8ELi1EE": (8, 1), "4TileILi2ELi2ELi4ELi4ELi2EE": (4, 2), "4TileILi4ELi1ELi1ELi4ELi4EE": (4, 4),
-            "fp8_rows_kernel": (8, 2), "fp8_reduce_kernel": (4, 8), "rotary_qkv_kernelIDF16bDF16b": (8, 2),
+            "ELi8ELi2ELi1EEEv": (8, 2), "ELi8ELi2ELi2EEEv": (8, 2), "ELi8ELi2ELi4EEEv": (8, 1), "fp8_reduce_kernel": (4, 8), "rotary_qkv_kernelIDF16bDF16b": (8, 2),
             "quantize_fp8_rows_kernel": (4, 5), "quantize_fp8_weight_kernel": (4, 6), "ln_modulate_fp8_kernel": (1, 8)}
 
 

@@ -35,7 +35,7 @@ def test_bounds():
         for exact in (False, True):
             tile, split, floats = fp8_form(m, n, k, exact, cus)
             seen.add((tile, exact, split > 1))
-            assert (tile == "rows") == (m <= 16) and (split == 1 or tile not in ("rows", "256x256"))
+            assert (tile == "rows") == (m <= 16 or m <= 32 and -(-n // 16) < 2 * cus) and (split == 1 or tile not in ("rows", "256x256"))
             assert not (exact and tile == "256x256")
             most = max(most, floats)
             if split == 1:

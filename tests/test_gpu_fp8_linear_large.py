@@ -18,7 +18,7 @@ LARGE = [(16640, 1536, 1536, "256x256", 1), (32760, 4608, 1536, "256x256", 1), (
          (300, 4608, 8960, "64x64", 1), (1000, 1536, 8960, "64x64", 1), (5000, 200, 144, "64x64", 1),
          (300, 4608, 1536, "64x64", 1), (600, 1001, 8976, "64x64", 3), (64, 1536, 8960, "64x64", 12),
          (1038, 1208, 13824, "128x128", 4), (1038, 1207, 13840, "128x128", 4),
-         (633, 1312, 6912, "64x64", 2), (633, 1309, 6928, "64x64", 2), (16, 28672, 1040, "rows", 1), (9, 1001, 8976, "rows", 1), (1, 8960, 1536, "rows", 1)]
+         (633, 1312, 6912, "64x64", 2), (633, 1309, 6928, "64x64", 2), (16, 28672, 1040, "rows", 1), (17, 4608, 1536, "rows", 1), (32, 1001, 8976, "rows", 1), (29, 8176, 400, "rows", 1), (32, 8960, 1536, "64x64", 1), (9, 1001, 8976, "rows", 1), (1, 8960, 1536, "rows", 1)]
 
 
 @pytest.mark.parametrize("m,n,k,tile,split", LARGE)
