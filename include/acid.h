@@ -578,7 +578,8 @@ acid_status acid_linear_w4(int32_t x_dtype, int64_t M, int32_t N, int32_t K, int
 /* e4m3 rows: codes [rows][K] of one byte (OCP e4m3: finite, up to 448), and for each
  * row and group of 128 inputs (the last may be shorter) an fp32 scale, value = code
  * scale; scales are laid out [ceil(K/128)][scales_ld], scales_ld >= round_up(rows, 4)
- * and a multiple of 4 (entries past `rows` are neither written nor used).
+ * and a multiple of 4 (entries past `rows` are neither written nor used; with no rows it
+ * may be anything).
  *   scale = max(max |x| / 448, 2^-126), code = x (1 / scale) to nearest, ties to even
  * A group with an infinity or a NaN gets scale NaN and codes that mean nothing.  K is a
  * multiple of 16, <= 2^22, ceil(rows / 32) ceil(K / 128) < 2^26; matrices' rows lie

@@ -747,7 +747,7 @@ acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t
   if (p.a_ld < K || p.a_ld % 16 || p.a_ld >= (1 << 24) || p.out_ld < N || p.out_ld > most ||
       (update && (p.residual_ld < N || p.residual_ld > most)))
     return set_error(ACID_ERR_SHAPE, "fp8: a_ld >= K, whole 16 bytes and < 2^24, out_ld and residual_ld >= N and <= 2^32");
-  if (p.a_scales_ld < round_up(M, 4) || p.a_scales_ld % 4 || p.a_scales_ld > most)
+  if (M > 0 && (p.a_scales_ld < round_up(M, 4) || p.a_scales_ld % 4 || p.a_scales_ld > most))
     return set_error(ACID_ERR_SHAPE, "fp8: a_scales_ld >= round_up(M, 4), a multiple of 4");
   if (M == 0) return ACID_OK;
   if (!p.a || !p.w || !p.a_scales || !p.w_scales || !p.out || (update && (!p.gate || !p.residual)))

@@ -248,7 +248,8 @@ acid_status check_rows(int64_t rows, int64_t K, int64_t x_ld, int64_t x_size, in
   if (x_ld < K || x_ld * x_size % 16 || x_ld > most || codes_ld < K || codes_ld % 16 ||
       codes_ld > most)
     return set_error(ACID_ERR_SHAPE, "fp8: rows at least K apart, whole 16 bytes, at most 2^32");
-  if (scales_ld < round_up(rows, 4) || scales_ld % 4 || scales_ld > most)
+  // (no rows have no scales: an empty matrix's stride means nothing)
+  if (rows > 0 && (scales_ld < round_up(rows, 4) || scales_ld % 4 || scales_ld > most))
     return set_error(ACID_ERR_SHAPE, "fp8: scales' rows are round_up(rows, 4) or more apart, a multiple of 4");
   return ACID_OK;
 }
