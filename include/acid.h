@@ -582,7 +582,7 @@ acid_status acid_linear_w4(int32_t x_dtype, int64_t M, int32_t N, int32_t K, int
  * may be anything).
  *   scale = max(max |x| / 448, 2^-126), code = x (1 / scale) to nearest, ties to even
  * A group with an infinity or a NaN gets scale NaN and codes that mean nothing.  K is a
- * multiple of 16, <= 2^22, ceil(rows / 32) ceil(K / 128) < 2^26; matrices' rows lie
+ * multiple of 16, <= 2^22, ceil(rows / 32) ceil(K / 128) < 2^26 - 3; matrices' rows lie
  * whole 16 bytes apart, buffers are 16-byte aligned and apart from one another.
  *
  * acid_quantize_fp8: rows x [rows][x_ld] in x_dtype. */

@@ -236,14 +236,15 @@ __global__ __launch_bounds__(256) void quantize_fp8_weight_kernel(const float* _
   }
 }
 
-// What every call on e4m3 rows asks of their layout.
+// What every call on e4m3 rows asks of their layout; of their number, that quantize_fp8_rows_kernel's
+// workgroups, four of those 32 x 128 tiles each, have fewer than 2^32 threads in all.
 acid_status check_rows(int64_t rows, int64_t K, int64_t x_ld, int64_t x_size, int64_t codes_ld,
                        int64_t scales_ld) {
   if (rows < 0 || K < 1) return set_error(ACID_ERR_INVALID_ARG, "fp8: rows < 0 or K < 1");
-  if (K % 16 || K > (1 << 22) || (rows + 31) / 32 * fp8_groups(K) >= (1 << 26))
+  if (K % 16 || K > (1 << 22) || (rows + 31) / 32 * fp8_groups(K) >= (1 << 26) - 3)
     return set_error(ACID_ERR_SHAPE,
                      "fp8: K %lld must be a multiple of 16, <= 2^22, and ceil(rows / 32) "
-                     "ceil(K / 128) < 2^26", (long long)K);
+                     "ceil(K / 128) < 2^26 - 3", (long long)K);
   constexpr int64_t most = (int64_t)1 << 32;
   if (x_ld < K || x_ld * x_size % 16 || x_ld > most || codes_ld < K || codes_ld % 16 ||
       codes_ld > most)
