@@ -676,8 +676,8 @@ typedef struct {
  * Contiguous q_out [n_seq][heads][tokens][d] is attention's; other strides write
  * into a cache's rows or keep tokens outermost, sequences beyond both.  q, k, v, q_out, k_out, weights and
  * biases 16-byte aligned, rows and strides of the first five whole 16 bytes; vt as its
- * elements.  Outputs apart from all else, but q_out may be q's own rows (of its type,
- * tokens outermost), k_out k's. */
+ * elements; the stride of an axis of one entry does not matter.  Outputs apart from all else,
+ * but q_out may be q's own rows (of its type, tokens outermost), k_out k's. */
 acid_status acid_rotary_qkv(const acid_rotary_qkv_args* args, int64_t n_seq, int64_t tokens,
                             hipStream_t stream);
 

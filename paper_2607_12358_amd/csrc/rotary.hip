@@ -392,7 +392,7 @@ acid_status acid_rotary_qkv(const acid_rotary_qkv_args* args, int64_t n_seq, int
   for (const auto& i : ins)
     if (i.in && (i.ld < i.width || i.ld * is % 16 || i.ld > most))
       return set_error(ACID_ERR_SHAPE, "rotary: rows at least heads * head_dim apart, whole 16 bytes, at most 2^32");
-  const struct {
+  struct {
     const void* out;
     int64_t heads, rows, width, head, row, seq;
   } outs[] = {{p.q_out, p.heads, tokens, d, p.q_head, p.q_row, p.q_seq},
@@ -400,10 +400,16 @@ acid_status acid_rotary_qkv(const acid_rotary_qkv_args* args, int64_t n_seq, int
               {p.vt, p.kv_heads, d, tokens, p.vt_head, p.vt_row, p.vt_seq}};
   if (rows == 0) return ACID_OK;
   for (int i = 0; i < 3; ++i) {
-    const auto& o = outs[i];
+    auto& o = outs[i];
     if (!o.out) continue;
     constexpr int64_t far = (int64_t)1 << 40;
-    if (o.head < 0 || o.row < 0 || o.seq < 0 || o.head > far || o.row > far || o.seq > far ||
+    auto out_of_range = [](int64_t n, int64_t stride) { return n > 1 && (stride < 0 || stride > far); };
+    bool bad = out_of_range(o.heads, o.head) || out_of_range(o.rows, o.row) || out_of_range(n_seq, o.seq);
+    // An axis of one entry may have any stride (a single token's heads are also its row's, one head's
+    // tokens the matrix's): it counts as the least that keeps the entries apart.
+    if (o.heads == 1) o.head = o.rows == 1 ? o.width : (o.rows - 1) * o.row + o.width;
+    if (o.rows == 1) o.row = (o.heads - 1) * o.head + o.width;
+    if (bad ||
         (i < 2 && (o.head * os % 16 || o.row * os % 16 || (n_seq > 1 && o.seq * os % 16))) ||
         !own_addresses(n_seq, o.heads, o.rows, o.width, o.head, o.row, o.seq))
       return set_error(ACID_ERR_SHAPE, "rotary: outputs' strides: values apart; of q_out and k_out whole 16 bytes");
@@ -443,8 +449,8 @@ acid_status acid_rotary_qkv(const acid_rotary_qkv_args* args, int64_t n_seq, int
     if (!o.out) continue;
     for (int j = 0; j < 9; ++j) {
       // Q and K may be turned in place: the same rows, of the same type
-      const bool same = i < 2 && j == i && o.out == ins[i].in && is == os && o.head == d && o.row == ins[i].ld &&
-                        (n_seq == 1 || o.seq == tokens * o.row);
+      const bool same = i < 2 && j == i && o.out == ins[i].in && is == os && (o.heads == 1 || o.head == d) &&
+                        (tokens == 1 || o.row == ins[i].ld) && (n_seq == 1 || o.seq == tokens * ins[i].ld);
       if (!same && overlap(written[i], inputs[j]))
         return set_error(ACID_ERR_INVALID_ARG, "rotary: an output overlaps an input");
     }
