@@ -17,7 +17,7 @@ from . import _lib as _L
 from ._lib import (ACID_BF16, ACID_CACHE_APPLY, ACID_CACHE_STORE, ACID_EPI_BIAS,  # noqa: F401
                    ACID_EPI_BIAS_GELU, ACID_EPI_EULER, ACID_EPI_GATE_RESIDUAL, ACID_EPI_QKV,
                    ACID_EPI_QKV_GELU, ACID_BLOCK_PARALLEL, ACID_BLOCK_SEQUENTIAL,
-                   ACID_F32, ACID_MODE_ACID, ACID_MODE_DICACHE, ACID_MODE_EASYCACHE,
+                   ACID_F32, ACID_FP8_EXACT, ACID_MODE_ACID, ACID_MODE_DICACHE, ACID_MODE_EASYCACHE,
                    ACID_HEAD_NORM_LAYER, ACID_HEAD_NORM_NONE, ACID_HEAD_NORM_RMS,
                    ACID_HEAD_NORM_RMS_ROW, ACID_MODE_NOCACHE, ACID_NORM_LAYER, ACID_NORM_NONE, ACID_NORM_RMS,
                    KERNEL_CLASSES, AcidError,
@@ -525,11 +525,14 @@ _FP8_ARGS = struct.Struct("@PqPqPPPPPqPqPNii")  # acid_linear_fp8_args
 
 
 def linear_fp8(a, a_scales, w, w_scales, out, bias=None, gelu: bool = False, gate=None, residual=None,
-               workspace=None, stream=None) -> None:
+               workspace=None, stream=None, exact: bool = False) -> None:
     """y = a w^T + bias of e4m3 rows a [m, k] (quantize_fp8, ln_modulate_fp8) and e4m3
     weights w [n, k] (quantize_fp8_weight); out [m, n], bf16 or fp32, is y, GELU(y) with
     gelu, or with gate (fp32 [n]) and residual (fp32 [m, n], out itself will do)
-    residual + gate y in fp32.  bias fp32 [n].  a, a_scales, residual and out may be
+    residual + gate y in fp32.  bias fp32 [n].  y in fp32 and GELU(y) in fp32 come from
+    exact products; bf16 outputs and the gated y from the 8-bit matrix units, which drop
+    what lies below 2^-13 of the largest of each eight products, or with exact from
+    exact ones too, in up to twice the time.  a, a_scales, residual and out may be
     row-strided.  workspace: uint8 tensor of linear_fp8_workspace bytes, kept by callers
     whose calls must not allocate; by default one is taken from torch's allocator."""
     torch, N, at, rows_at = _native()
@@ -555,7 +558,8 @@ def linear_fp8(a, a_scales, w, w_scales, out, bias=None, gelu: bool = False, gat
         *((0, 0) if residual is None else rows_at(dev, "residual", residual, (m, n), f32)),
         *rows_at(dev, "out", out, (m, n), out.dtype),
         0 if workspace is None else at(dev, "workspace", workspace, (size,), torch.uint8), size,
-        ACID_EPI_GATE_RESIDUAL if gate is not None else ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS,
+        (ACID_EPI_GATE_RESIDUAL if gate is not None else ACID_EPI_BIAS_GELU if gelu else ACID_EPI_BIAS)
+        | (ACID_FP8_EXACT if exact else 0),
         _dtype_code(torch, out, "out"))
     _on(torch, dev, stream, N.linear_fp8, args, m, n, k)
 

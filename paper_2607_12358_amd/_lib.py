@@ -25,6 +25,7 @@ ACID_CACHE_STORE, ACID_CACHE_APPLY = 0, 1
  ACID_EPI_EULER, ACID_EPI_QKV_GELU) = range(6)
 ACID_BLOCK_SEQUENTIAL, ACID_BLOCK_PARALLEL = 0, 1
 ACID_NORM_NONE, ACID_NORM_LAYER, ACID_NORM_RMS = 0, 1, 2
+ACID_FP8_EXACT = 0x100
 (ACID_HEAD_NORM_NONE, ACID_HEAD_NORM_LAYER, ACID_HEAD_NORM_RMS,
  ACID_HEAD_NORM_RMS_ROW) = range(4)
 KERNEL_CLASSES = ("temb", "ln_mod", "gemm_qkv", "attention", "gemm_proj", "gemm_ffn1",

@@ -9,14 +9,17 @@
 // register.
 //
 // Two forms of the inner sum.  The 8-bit matrix instructions add eight neighbouring
-// products at a time, aligned to the largest of them and cut below 2^-13 of it
-// (measured; both the 32x32x64 and the older 32x32x16 do): random operands give sums
-// that are 1.4e-5 off, against 2^-9 for the rounding to bf16 that follows and some 2^-5
-// for the operands' own.  Outputs in bf16, and updates of a residual, take them.
-// Plain fp32 outputs take the bf16 instruction on operands converted on the way, which
-// is exact: products and sums in fp32, in about twice the time (32760 x 1536 x 8960 773 us
-// for 367).  For the update of a residual that would be more than acid_linear's on bf16
-// operands takes (660 us), and y's operands have lost far more.
+// products at a time, aligned to the largest of them, and drop towards zero what lies below
+// 2^-13 of it (measured; both the 32x32x64 and the older 32x32x16 do): 7 2^-13 of the
+// largest product at most.  Random operands give sums that are 1.4e-5 off, to no side;
+// operands of one sign, sums 2.5e-6 too small.  The rounding to bf16 that may follow is 2^-9, and
+// the operands' own are some 2^-5.  Outputs in bf16, and updates of a residual, take them.
+// Plain fp32 outputs, and with ACID_FP8_EXACT all, take the bf16 instruction on operands
+// converted on the way, which is exact: products and sums in fp32, in up to twice the time
+// (us, 32760 x 1536 x 8960: bf16 759 for 368, fp32 776, onto a residual 826 for 447; x 1536 x
+// 1536 onto a residual 180 for 130; 64 x 1536 x 8960 15.0 for 12.9).  An update of a residual
+// costs more so than by acid_linear on operands of 16 bits (660 us), so exact ones are for
+// who asks for them: they keep small products beside an outlier, or beside two that cancel.
 //
 // Microseconds on one MI355X, 8-bit products to bf16 (a register-only stream of the
 // instruction makes 3.8 PFLOP/s, the library's product without block scales 2.4 to 3.3):
@@ -733,9 +736,10 @@ acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t
   const acid_linear_fp8_args& p = *args;
   if (p.out_dtype != ACID_F32 && p.out_dtype != ACID_BF16)
     return set_error(ACID_ERR_INVALID_ARG, "bad dtype %d", p.out_dtype);
-  const bool update = p.kind == ACID_EPI_GATE_RESIDUAL;
-  if (p.kind != ACID_EPI_BIAS && p.kind != ACID_EPI_BIAS_GELU && !update)
-    return set_error(ACID_ERR_UNSUPPORTED, "fp8: epilogue %d is not BIAS, BIAS_GELU or GATE_RESIDUAL", p.kind);
+  const int32_t kind = p.kind & ~ACID_FP8_EXACT;
+  const bool update = kind == ACID_EPI_GATE_RESIDUAL;
+  if (kind != ACID_EPI_BIAS && kind != ACID_EPI_BIAS_GELU && !update)
+    return set_error(ACID_ERR_UNSUPPORTED, "fp8: epilogue %d is not BIAS, BIAS_GELU or GATE_RESIDUAL", kind);
   if (update && p.out_dtype != ACID_F32)
     return set_error(ACID_ERR_UNSUPPORTED, "fp8: GATE_RESIDUAL writes fp32");
   if (M < 0 || N < 1 || K < 1) return set_error(ACID_ERR_INVALID_ARG, "M < 0, N < 1 or K < 1");
@@ -791,14 +795,17 @@ acid_status acid_linear_fp8(const acid_linear_fp8_args* args, int64_t M, int32_t
   const Fp8Args a = {(const uint8_t*)p.a, (const uint8_t*)p.w, p.a_scales, p.w_scales, p.bias, p.gate,
                      p.residual, p.out, p.a_ld, p.a_scales_ld, p.residual_ld, p.out_ld, (float*)p.workspace, (int32_t)M, N,
                      K, (int32_t)groups, 1, whole, wide};
+  // 8-bit sums where a rounding to bf16 follows or the residual outweighs them, exact ones where asked for
+  const bool exact = p.kind & ACID_FP8_EXACT;
   hipError_t e;
-  if (p.out_dtype == ACID_BF16)
-    e = p.kind == ACID_EPI_BIAS ? launch<bf16, ACID_EPI_BIAS, false>(a, stream)
-                                : launch<bf16, ACID_EPI_BIAS_GELU, false>(a, stream);
+  if (update)
+    e = exact ? launch<float, ACID_EPI_GATE_RESIDUAL, true>(a, stream) : launch<float, ACID_EPI_GATE_RESIDUAL, false>(a, stream);
+  else if (p.out_dtype == ACID_F32)
+    e = kind == ACID_EPI_BIAS ? launch<float, ACID_EPI_BIAS, true>(a, stream) : launch<float, ACID_EPI_BIAS_GELU, true>(a, stream);
+  else if (exact)
+    e = kind == ACID_EPI_BIAS ? launch<bf16, ACID_EPI_BIAS, true>(a, stream) : launch<bf16, ACID_EPI_BIAS_GELU, true>(a, stream);
   else
-    e = update                      ? launch<float, ACID_EPI_GATE_RESIDUAL, false>(a, stream)
-        : p.kind == ACID_EPI_BIAS ? launch<float, ACID_EPI_BIAS, true>(a, stream)
-                                  : launch<float, ACID_EPI_BIAS_GELU, true>(a, stream);
+    e = kind == ACID_EPI_BIAS ? launch<bf16, ACID_EPI_BIAS, false>(a, stream) : launch<bf16, ACID_EPI_BIAS_GELU, false>(a, stream);
   return e == hipSuccess ? ACID_OK : check_hip(e, "linear fp8");
 }
 
