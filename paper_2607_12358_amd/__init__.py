@@ -592,7 +592,11 @@ def rotary_qkv(q, k, v, positions, freqs, sections: Sequence[int], q_out, k_out,
         raise ValueError(f"unknown norm {norm!r}")
     if pairs not in _PAIRINGS:
         raise ValueError(f"unknown pairs {pairs!r}")
-    if not 1 <= len(sections) <= 4:
+    try:
+        axes, n_pairs = len(sections), sum(sections)
+    except TypeError:
+        raise ValueError(f"sections: expected numbers of pairs, got {sections!r}") from None
+    if not 1 <= axes <= 4:
         raise ValueError("sections: one to four axes")
     if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (vt is None):
         raise ValueError("q and q_out, k and k_out, v and vt go together")
@@ -609,6 +613,8 @@ def rotary_qkv(q, k, v, positions, freqs, sections: Sequence[int], q_out, k_out,
         raise ValueError(f"{rows} rows for {n_seq} sequences of {tokens} tokens")
     heads = q_out.shape[-3] if q is not None else 0
     kv_out = k_out if k is not None else vt
+    if kv_out is not None and kv_out.dim() != out.dim():
+        raise ValueError(f"{'vt' if k is None else 'k_out'}: expected {out.dim()} axes, as the other outputs have")
     kv_heads = kv_out.shape[-3] if kv_out is not None else 0
     nothing, no_heads = (0, 0), (0, 0, 0, 0)
     q_at, q_ld = nothing if q is None else rows_at(dev, "q", q, (rows, heads * d), dt)
@@ -618,9 +624,10 @@ def rotary_qkv(q, k, v, positions, freqs, sections: Sequence[int], q_out, k_out,
     qo = no_heads if q is None else N_heads(dev, "q_out", q_out, lead + (heads, tokens, d), odt)
     ko = no_heads if k is None else N_heads(dev, "k_out", k_out, lead + (kv_heads, tokens, d), odt)
     vo = no_heads if v is None else N_heads(dev, "vt", vt, lead + (kv_heads, d, tokens), odt)
-    axes, n_pairs = len(sections), sum(sections)
     where = pos_ld = turns = 0
     if n_pairs and (q is not None or k is not None):
+        if positions is None or freqs is None:
+            raise ValueError("positions and freqs: pairs need both")
         pdt = positions.dtype
         if pdt is not torch.int32 and pdt is not f32:
             raise ValueError(f"positions: expected int32 or float32, got {pdt}")
@@ -631,14 +638,17 @@ def rotary_qkv(q, k, v, positions, freqs, sections: Sequence[int], q_out, k_out,
             pos_ld = max(pos_ld, rows)
         turns = at(dev, "freqs", freqs, (n_pairs,), torch.float64)
     each = norm == "rms_row"
-    a = _ROTARY_ARGS.pack(
-        q_at, k_at, v_at, q_ld, k_ld, v_ld, qo[0], ko[0], vo[0], *qo[1:], *ko[1:], *vo[1:], where, pos_ld, turns,
-        at(dev, "q_weight", q_weight, (heads * d if each else d,), f32) or 0,
-        at(dev, "k_weight", k_weight, (kv_heads * d if each else d,), f32) or 0,
-        at(dev, "q_bias", q_bias, (d,), f32) or 0, at(dev, "k_bias", k_bias, (d,), f32) or 0,
-        _dtype_code(torch, some, "q, k and v"), _dtype_code(torch, out, "q_out, k_out and vt"),
-        heads, kv_heads, d, axes, *sections, *(0,) * (4 - axes), _PAIRINGS[pairs], _HEAD_NORMS[norm],
-        int(where != 0 and pdt is f32), q_scale, eps)
+    norms = (at(dev, "q_weight", q_weight, (heads * d if each else d,), f32) or 0,
+             at(dev, "k_weight", k_weight, (kv_heads * d if each else d,), f32) or 0,
+             at(dev, "q_bias", q_bias, (d,), f32) or 0, at(dev, "k_bias", k_bias, (d,), f32) or 0)
+    in_code, out_code = _dtype_code(torch, some, "q, k and v"), _dtype_code(torch, out, "q_out, k_out and vt")
+    try:
+        a = _ROTARY_ARGS.pack(
+            q_at, k_at, v_at, q_ld, k_ld, v_ld, qo[0], ko[0], vo[0], *qo[1:], *ko[1:], *vo[1:], where, pos_ld, turns,
+            *norms, in_code, out_code, heads, kv_heads, d, axes, *sections, *(0,) * (4 - axes), _PAIRINGS[pairs],
+            _HEAD_NORMS[norm], int(where != 0 and pdt is f32), q_scale, eps)
+    except (struct.error, OverflowError) as e:
+        raise ValueError(f"sections {sections!r}, q_scale {q_scale!r} and eps {eps!r}: {e}") from None
     _on(torch, dev, stream, N.rotary_qkv, a, n_seq, tokens)
 
 
