@@ -21,14 +21,15 @@ constexpr int kFp8FewRows = 16;
 // round that is not full counts in part; a split adds a second launch and its bytes.  The
 // constants are those that lose least against the best form of each of 185 measured shapes,
 // 17 to 16000 rows, N 64 to 9600, K 128 to 8960: 0.7% on average (exact products 1.7%), 11% at most
-// (28%); 256 x 256 tiles alone lose a factor of two.  Microseconds, 256 / 128 / 64, and
-// 64 in parts:
-//     64 x 1536 x 8960:  88.5 /  40.8 / 27.5, 64 in 8 parts 11.9
-//    300 x 1536 x 8960:  91.6 /  42.0 / 27.9, 64 in 4 parts 18.3
-//    600 x 4608 x 1536:  22.9 /  11.6 / 11.2, 64 in 2 parts 25.2
-//   2500 x 4608 x 8960: 104.4 / 108.5 / 173.0
-//   4096 x 4608 x 1536:  47.5 /  35.9 / 52.3
-//   8200 x 1536 x 8960: 110.2 / 128.8 / 190.3
+// (28%); 256 x 256 tiles alone lose a factor of two.  Microseconds in a graph, weights in turn,
+// 256 / 128 / 64, parts, and what the rule takes:
+//     64 x 1536 x 8960:  89.5 /  42.0 /  28.6, 64 in 4 parts 13.2, 8 11.5, 12 12.7: 64 in 12
+//    300 x 1536 x 8960:  92.7 /  42.8 /  29.1, 64 in 2 parts 20.8, 4 17.8, 8 19.6: 64 in 4
+//    600 x 4608 x 1536:  23.4 /  11.8 /  11.5, 64 in 2 parts 25.3: 64
+//   2048 x 1536 x 8960:  93.5 /  44.1 /  47.0, 128 in 2 parts 48.0, 3 53.3: 128 in 2
+//   2500 x 4608 x 8960: 102.3 / 114.2 / 182.5: 256
+//   4096 x 4608 x 1536:  47.2 /  36.8 /  53.6: 128
+//   8200 x 1536 x 8960: 109.0 / 131.2 / 191.1: 256
 // (64 x 128 tiles too would gain 0.8% on average; exact products, whose operands take twice the
 // registers, in 256 x 128 tiles nothing.)  Up to 16 rows have a kernel of their own, and up to
 // 32 where its workgroups, of 16 outputs and one a CU, take less than two rounds (its bf16

@@ -22,16 +22,20 @@
 // who asks for them: they keep small products beside an outlier, or beside two that cancel.
 //
 // Microseconds on one MI355X, 8-bit products to bf16 (a register-only stream of the
-// instruction makes 3.8 PFLOP/s, the library's product without block scales 2.4 to 3.3):
+// instruction makes 3.8 PFLOP/s, the library's product without block scales 2.4 to 3.3); the
+// last line in a graph, the others calls in a row:
 //   32760 x 4608 x 1536   227 (2.04 PFLOP/s)     8192 x 8192 x 8192  426 (2.58)
 //   32760 x 1536 x 8960   367 (2.46); onto a residual in fp32 445
-//   64 x 1536 x 8960  12.5   1 x 8960 x 1536  4.7    1 x 28672 x 8192  38.8 (6.1 TB/s)
-// The large ones run at 1.8 GHz with the matrix units 60% busy (the library's: 1.7 and
-// 82%).  At 32760 x 1536 x 8960 every part that was left out for a timing took its time with it,
-// whatever else was left out: loads of operands 15%, reads of LDS 20%, the scales'
-// multiply-adds 8%, barriers 3%, the outputs 6%.  Leaving out the waits, wave priorities
-// and other orders of the loads change nothing.  So the bound is what all of them share,
-// most likely the power of the card, and not a latency.
+//   64 x 1536 x 8960  12.7   1 x 8960 x 1536  4.7    1 x 28672 x 8192  38.8 (6.1 TB/s)
+// What bounds the large ones is cycles around the products.  At 32760 x 1536 x 8960 the matrix
+// units are busy 61% of 5.7 M active cycles, the library's 81% of 4.25 M; our waves wait 26%
+// of theirs, the library's 8%, with 11.3 M instructions of LDS for 6.9 M and 77 M of the
+// vector units for 18 M (32760 x 4608 x 1536: 48% for 55%, and with a residual 47% of 7.4 M).  The clock is
+// the power's, 1.6 to 1.9 GHz for both.  Parts left out for a timing took their time with
+// them: loads of operands 15%, reads of LDS 20%, the scales' multiply-adds 8%, barriers 3%,
+// the outputs 6%; leaving out the waits, wave priorities and other orders of the loads change
+// nothing.  By the two bf16 times a stage is 1.67 us and a tile 5 more.  Four waves of 128 x 128 each
+// would read a third less of LDS; that form has not been measured.
 
 #include <algorithm>
 #include <type_traits>
@@ -649,7 +653,7 @@ hipError_t launch_rows(const Fp8Args& a, hipStream_t s) {
 
 // The parts' sums of a split tile, added in order, then its outputs: four a thread.  Costs
 // some 3.3 us, its launch for the most part, where the split saves more (64 x 1536 x 8960 in
-// 64 x 64 tiles 27.5 -> 11.9 us).
+// 64 x 64 tiles 28.6 us, in twelve parts 12.7).
 template <typename Out, int KIND, typename T>
 __global__ __launch_bounds__(256) void fp8_reduce_kernel(Fp8Args a) {
   constexpr int EACH = T::TM * T::TN / 4, THREADS = 64 * T::WAVES;
